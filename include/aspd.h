@@ -305,6 +305,40 @@ int aspd_kv_append(aspd_plan_t* plan, const void* k_new /*device*/, const void* 
                    const int32_t* pos /*device*/, void* k_pool /*device*/, void* v_pool /*device*/,
                    void* stream);
 
+/* Options of aspd_qk_norm_append (host memory, read before the call returns). */
+typedef struct {
+  const void* q_weight; /* device [head_dim], element type of the shape, 16-byte aligned: gains of the queries' RMS norm;
+                           NULL: queries are not normalised                                   */
+  const void* k_weight; /* the same for the keys                                              */
+  float eps;            /* added to the mean square of a head; finite, >= 0                   */
+  int32_t n_axes;       /* position IDs per token: 1 to ASPD_MAX_AXES                         */
+  int32_t rotate_q;     /* 1: q_out is normalised and rotated (for plans of aspd_plan_create_scores with rotated = 1);
+                           0: q_out is normalised only (for plans whose attention rotates the queries itself)   */
+  uint8_t axis_of_pair[64]; /* which of a token's position IDs turns elements i and i + head_dim / 2, i < head_dim / 2 */
+} aspd_qk_norm_t;
+#define ASPD_MAX_AXES 4
+
+/*
+ * What a model with normalised heads or several position axes does between its projection and the
+ * attention, in one pass over the step's new tokens:
+ *   y = x / sqrt(mean(x^2) + eps) * weight   over each head of q and of k_new (where a weight is given)
+ *   RoPE: pair i of a head turned by pos[axis_of_pair[i]][t] * theta^(-2i/head_dim); keys always, queries
+ *   with rotate_q
+ * and the queries go to q_out, keys and values into the paged cache at the slots of the plan (as
+ * aspd_kv_append).  Sums, norms and rotation are fp32 with the angle reduced in fp64; one rounding to the
+ * storage type at the end.  The attention call of the same plan reads both.
+ *   q, k_new, v_new  rows of n_q_heads / n_kv_heads heads, head_dim elements each, lying together; *_stride
+ *                    elements from one token to the next (a multiple of 16 bytes, at least a row), so that
+ *                    the three may be views of one packed projection
+ *   pos              [n_axes][n_new] position IDs
+ *   q_out            [n_new][n_q_heads][head_dim]; may be q itself when q_stride is a row.  Nothing else may
+ *                    overlap.
+ */
+int aspd_qk_norm_append(aspd_plan_t* plan, const aspd_qk_norm_t* norm /*host*/, const void* q /*device*/, int64_t q_stride,
+                        const void* k_new /*device*/, int64_t k_stride, const void* v_new /*device*/, int64_t v_stride,
+                        const int32_t* pos /*device*/, void* k_pool /*device*/, void* v_pool /*device*/,
+                        void* q_out /*device*/, void* stream);
+
 /*
  * a4-a7: parallel-mode attention (Eq. 1 under the mask of Eq. 2-3).  Query i of branch b
  * attends the prefix [0, P) and tokens 0 .. kv_len - q_len + i of its own branch; the prefix

@@ -55,6 +55,14 @@ class PlanInfo(ctypes.Structure):
                 ("algorithmic_bytes", ctypes.c_int64)]
 
 
+MAX_AXES = 4
+
+
+class _QkNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("n_axes", ctypes.c_int32),
+                ("rotate_q", ctypes.c_int32), ("axis_of_pair", ctypes.c_uint8 * 64)]
+
+
 class AspdError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -64,7 +72,7 @@ class AspdError(RuntimeError):
 EXPORTS = ("aspd_strerror", "aspd_pool_bytes", "aspd_count_new_tokens", "aspd_positions", "aspd_visible_slots",
            "aspd_visible_slots_masked", "aspd_plan_create", "aspd_plan_update", "aspd_plan_destroy", "aspd_release_cached_memory", "aspd_plan_info", "aspd_plan_items", "aspd_plan_cta_ranges", "aspd_plan_stream_pages",
            "aspd_plan_token_ranges", "aspd_plan_shared_mask_tables", "aspd_plan_status",
-           "aspd_kv_append", "aspd_branch_attn", "aspd_serial_attn", "aspd_attn_partials", "aspd_attn_combine", "aspd_step_partials",
+           "aspd_kv_append", "aspd_qk_norm_append", "aspd_branch_attn", "aspd_serial_attn", "aspd_attn_partials", "aspd_attn_combine", "aspd_step_partials",
            "aspd_branch_step", "aspd_serial_step", "aspd_step_host", "aspd_step_host_async", "aspd_attn_static", "aspd_static_status", "aspd_k_rerotate", "aspd_k_rerotate_ranges", "aspd_k_rerotate_ranges_layers", "aspd_debug_read_token", "aspd_debug_bounded_wait", "aspd_debug_profile", "aspd_debug_pool_limit")
 
 _lib = None
@@ -104,6 +112,8 @@ def lib() -> ctypes.CDLL:
         L.aspd_plan_shared_mask_tables.argtypes = [vp, vp, vp]
         L.aspd_plan_status.argtypes = [vp, vp]
         L.aspd_kv_append.argtypes = [vp] * 7
+        i64 = ctypes.c_int64
+        L.aspd_qk_norm_append.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp]
         L.aspd_branch_attn.argtypes = [vp] * 6
         L.aspd_serial_attn.argtypes = [vp] * 6
         L.aspd_attn_partials.argtypes = [vp] * 5
@@ -300,6 +310,57 @@ class Plan:
 def kv_append(plan: Plan, k_new, v_new, pos, k_pool, v_pool, stream=None) -> None:
     _check(lib().aspd_kv_append(plan._h, _ptr(k_new), _ptr(v_new), _ptr(pos), _ptr(k_pool), _ptr(v_pool), _stream(stream)),
            "aspd_kv_append")
+
+
+def axes_of_pairs(sections, interleaved: bool = False):
+    """``axis_of_pair`` of a model whose axes take ``sections`` pairs each: one after another, or taking turns
+    (axis a > 0 has pairs a, a + n, ... as far as its section goes, axis 0 the rest)."""
+    n, half = len(sections), sum(sections)
+    if not interleaved:
+        return [a for a, m in enumerate(sections) for _ in range(m)]
+    return [i % n if i % n and i // n < sections[i % n] else 0 for i in range(half)]
+
+
+class QkNorm:
+    """What ``qk_norm_append`` does to a layer's queries and keys (``aspd_qk_norm_t``): the gains of the norms (device
+    tensors of the storage type, [head_dim]; None: not normalised), eps, which position axis turns which pair."""
+
+    def __init__(self, shape: Shape, q_weight=None, k_weight=None, eps: float = 1e-6, axis_of_pair=None, rotate_q: bool = False):
+        half, axes = shape.head_dim // 2, [0] * (shape.head_dim // 2) if axis_of_pair is None else [int(a) for a in axis_of_pair]
+        if len(axes) != half or not all(0 <= a < MAX_AXES for a in axes):
+            raise ValueError(f"axis_of_pair: {half} numbers from 0 to {MAX_AXES - 1}")
+        for w in (q_weight, k_weight):
+            if w is not None and (w.numel() != shape.head_dim or not w.is_contiguous() or w.element_size() != _esize(shape)):
+                raise ValueError("weights: head_dim contiguous elements of the storage type")
+        self.weights = q_weight, k_weight           # kept alive
+        self.n_axes = max(axes) + 1
+        self.c = _QkNorm(_ptr(q_weight), _ptr(k_weight), eps, self.n_axes, 1 if rotate_q else 0, (ctypes.c_uint8 * 64)(*axes))
+
+
+def _esize(shape: Shape) -> int:
+    return 2 if shape.dtype == DTYPE_BF16 else 4
+
+
+def _token_stride(x, shape: Shape, heads: int, n: int) -> int:
+    """Elements from one token's heads to the next one's; the heads of a token must lie together."""
+    row = heads * shape.head_dim
+    inner = x.stride()[1:] == (shape.head_dim, 1) if x.dim() == 3 else x.dim() == 2 and x.stride(1) == 1
+    if x.shape[0] != n or x.numel() != n * row or not (inner or (x.dim() == 3 and heads == 1 and x.stride(2) == 1)) or x.element_size() != _esize(shape):
+        raise ValueError("tokens: [n_new][heads][head_dim] of the storage type, the heads of a token together")
+    return x.stride(0) if n > 1 else row
+
+
+def qk_norm_append(plan: Plan, norm: QkNorm, q, k_new, v_new, pos, k_pool, v_pool, q_out, stream=None) -> None:
+    """Norms, rotation and paged append of the step's new tokens (see ``aspd_qk_norm_append``).  q, k_new, v_new may be
+    views of one packed projection; pos: device int32 [n_axes][n_new]."""
+    sh, n = plan.shape, plan.n_new
+    if pos.numel() < norm.n_axes * n or not pos.is_contiguous() or pos.element_size() != 4:
+        raise ValueError("pos: contiguous int32 [n_axes][n_new]")
+    strides = [_token_stride(x, sh, h, n) for x, h in ((q, sh.n_q_heads), (k_new, sh.n_kv_heads), (v_new, sh.n_kv_heads))]
+    if q_out.numel() != n * sh.n_q_heads * sh.head_dim or not q_out.is_contiguous() or q_out.element_size() != _esize(sh):
+        raise ValueError("q_out: contiguous [n_new][n_q_heads][head_dim] of the storage type")
+    _check(lib().aspd_qk_norm_append(plan._h, ctypes.addressof(norm.c), _ptr(q), strides[0], _ptr(k_new), strides[1], _ptr(v_new), strides[2],
+                                     _ptr(pos), _ptr(k_pool), _ptr(v_pool), _ptr(q_out), _stream(stream)), "aspd_qk_norm_append")
 
 
 def branch_attn(plan: Plan, q, k_pool, v_pool, out, stream=None) -> None:

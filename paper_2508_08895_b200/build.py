@@ -14,7 +14,7 @@ LIB_DEBUG_BOUNDS = os.path.join(HERE, "libaspd_debug_bounds.so")   # -DASPD_DEBU
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+    "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
 

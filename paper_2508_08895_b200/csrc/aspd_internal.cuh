@@ -187,6 +187,8 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
 // launchers (each returns an aspd_status_t)
 int launch_append(const aspd_plan* p, const void* k_new, const void* v_new, const int32_t* pos,
                   void* k_pool, void* v_pool, cudaStream_t s);
+int launch_qk_norm(const aspd_plan* p, const aspd_qk_norm_t* nm, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                   const void* v_new, int64_t v_stride, const int32_t* pos, void* k_pool, void* v_pool, void* q_out, cudaStream_t s);
 // k_new / v_new non-null: the step's new rows are written first
 int launch_attn_generic(const aspd_plan* p, const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool,
                         cudaStream_t s);

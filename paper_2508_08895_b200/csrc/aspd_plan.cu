@@ -1,5 +1,6 @@
 // Host side of the library: descriptor validation, position IDs and slots (integer rules of
 // Eq. 4 and Section 3.3), the split-K work list, plan life cycle and the C entry points.
+#include <float.h>
 #include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -1207,6 +1208,27 @@ int aspd_kv_append(aspd_plan_t* p, const void* k_new, const void* v_new, const i
   if (!k_new || !v_new || !pos || !k_pool || !v_pool || misaligned16(k_new, v_new, k_pool, v_pool)) return ASPD_ERR_INVALID_ARG;
   note_stream(p, stream);
   return launch_append(p, k_new, v_new, pos, k_pool, v_pool, (cudaStream_t)stream);
+}
+
+int aspd_qk_norm_append(aspd_plan_t* p, const aspd_qk_norm_t* nm, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                        const void* v_new, int64_t v_stride, const int32_t* pos, void* k_pool, void* v_pool, void* q_out, void* stream) {
+  if (!p || p->host_only || !nm) return ASPD_ERR_INVALID_ARG;
+  const aspd_shape_t& sh = p->shape;
+  if (!(nm->eps >= 0.f) || !(nm->eps <= FLT_MAX) || nm->n_axes < 1 || nm->n_axes > ASPD_MAX_AXES || misaligned16(nm->q_weight, nm->k_weight))
+    return ASPD_ERR_INVALID_ARG;
+  for (int i = 0; i < sh.head_dim / 2; ++i)
+    if (nm->axis_of_pair[i] >= nm->n_axes) return ASPD_ERR_INVALID_ARG;
+  if (p->n_new == 0) return ASPD_OK;
+  if (!q || !k_new || !v_new || !pos || !k_pool || !v_pool || !q_out || misaligned16(q, k_new, v_new, k_pool, v_pool, q_out))
+    return ASPD_ERR_INVALID_ARG;
+  if (p->n_new > 1) {                              // (a single token has no next one)
+    const int64_t unit = 16 / esize_of(sh.dtype), q_row = (int64_t)sh.n_q_heads * sh.head_dim, kv_row = (int64_t)sh.n_kv_heads * sh.head_dim;
+    if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row || q_stride % unit || k_stride % unit || v_stride % unit ||
+        (q_out == q && q_stride != q_row))
+      return ASPD_ERR_INVALID_ARG;
+  }
+  note_stream(p, stream);
+  return launch_qk_norm(p, nm, q, q_stride, k_new, k_stride, v_new, v_stride, pos, k_pool, v_pool, q_out, (cudaStream_t)stream);
 }
 
 int aspd_attn_partials(aspd_plan_t* p, const void* q, const void* k_pool, const void* v_pool, void* stream) {
