@@ -248,6 +248,37 @@ int aspd_plan_create(const aspd_shape_t* shape, const aspd_request_t* req, const
                      const int32_t* q_pos, const aspd_tuning_t* tuning, void* stream,
                      aspd_plan_t** plan_out);
 /*
+ * Plans whose attention scores are not the plain scaled products (model families whose attention caps its
+ * scores, or has no rotation but a bias that falls with distance), or whose queries and keys come rotated:
+ *
+ *   logit(i, j) = f(sm_scale * q_i . k_j) - slopes[query head] * (pos(i) - pos(j)),   f(x) = cap * tanh(x / cap)
+ *
+ * Every attention and step call takes such a plan (also aspd_plan_update and host-only plans for
+ * aspd_attn_static).  The position IDs of the bias are those of the descriptors (aspd_positions), whatever
+ * q_pos says: slot s of the prefix has position s, token k of a branch pos_start + k (ASPD_POS_AUTO: Eq. 4), in
+ * serial mode too, token k of the tail prefix_len + the sum of all kv_len + k.  Regions of earlier stages
+ * (ASPD_Q_SHARED) have the positions they were written at, which only the caller knows: with slopes their
+ * pos_start must be given (ASPD_ERR_BAD_DESCRIPTOR for ASPD_POS_AUTO).
+ */
+typedef struct {
+  float cap;           /* > 0: scores are capped; 0: they are not                                      */
+  const float* slopes; /* host [n_q_heads], read before the call returns; NULL: no bias         */
+  int32_t rotated;     /* 1: q and k_new come as they are to be used (aspd_qk_norm_append with rotate_q, or a model
+                          without rotation): the attention and the fused step rotate nothing (the plan's q_pos are all
+                          0; a caller's are refused).  Their elements must be finite.  aspd_kv_append still rotates by
+                          the positions it is given                                                     */
+} aspd_scores_t;
+/*
+ * aspd_plan_create with these options (scores = NULL: the same).  ASPD_ERR_INVALID_ARG for a cap that is
+ * negative, above 1e30, or below sm_scale / 1e30; for slopes above 1e30 in magnitude or not finite; for q_pos with
+ * rotated.  ASPD_ERR_UNSUPPORTED for a cap or slopes with tuning->mma_m = 64.  With slopes, ASPD_ERR_TOO_LARGE for
+ * position IDs of 2^24 and more.
+ */
+int aspd_plan_create_scores(const aspd_shape_t* shape, const aspd_request_t* req, const aspd_branch_t* br,
+                            const int32_t* page_ids, int n_req, int64_t n_pool_pages, int mode,
+                            const int32_t* q_pos, const aspd_tuning_t* tuning, const aspd_scores_t* scores, void* stream,
+                            aspd_plan_t** plan_out);
+/*
  * Destroys the plan.  Work of the plan that is still in flight need not be waited for: the plan's
  * device block is parked with an event recorded on every stream the plan was used on, and a later
  * aspd_plan_create reuses a parked block of fitting size after making its own stream wait for

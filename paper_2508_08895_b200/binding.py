@@ -63,6 +63,24 @@ class _QkNorm(ctypes.Structure):
                 ("rotate_q", ctypes.c_int32), ("axis_of_pair", ctypes.c_uint8 * 64)]
 
 
+class _Scores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("rotated", ctypes.c_int32)]
+
+
+class Scores:
+    """Scores that are not the plain scaled products (``aspd_scores_t``): capped by cap * tanh(x / cap), lowered by
+    slopes[query head] per position of distance; ``rotated``: queries and keys come as they are to be used."""
+
+    def __init__(self, cap: float = 0.0, slopes=None, rotated: bool = False):
+        self.slopes = None if slopes is None else np.ascontiguousarray(slopes, dtype=np.float32)
+        self.cap, self.rotated = cap, rotated
+
+    def c_struct(self, shape: "Shape") -> _Scores:
+        if self.slopes is not None and self.slopes.shape != (shape.n_q_heads,):
+            raise ValueError("slopes: one per query head")
+        return _Scores(self.cap, None if self.slopes is None else self.slopes.ctypes.data, 1 if self.rotated else 0)
+
+
 class AspdError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -70,7 +88,7 @@ class AspdError(RuntimeError):
 
 
 EXPORTS = ("aspd_strerror", "aspd_pool_bytes", "aspd_count_new_tokens", "aspd_positions", "aspd_visible_slots",
-           "aspd_visible_slots_masked", "aspd_plan_create", "aspd_plan_update", "aspd_plan_destroy", "aspd_release_cached_memory", "aspd_plan_info", "aspd_plan_items", "aspd_plan_cta_ranges", "aspd_plan_stream_pages",
+           "aspd_visible_slots_masked", "aspd_plan_create", "aspd_plan_create_scores", "aspd_plan_update", "aspd_plan_destroy", "aspd_release_cached_memory", "aspd_plan_info", "aspd_plan_items", "aspd_plan_cta_ranges", "aspd_plan_stream_pages",
            "aspd_plan_token_ranges", "aspd_plan_shared_mask_tables", "aspd_plan_status",
            "aspd_kv_append", "aspd_qk_norm_append", "aspd_branch_attn", "aspd_serial_attn", "aspd_attn_partials", "aspd_attn_combine", "aspd_step_partials",
            "aspd_branch_step", "aspd_serial_step", "aspd_step_host", "aspd_step_host_async", "aspd_attn_static", "aspd_static_status", "aspd_k_rerotate", "aspd_k_rerotate_ranges", "aspd_k_rerotate_ranges_layers", "aspd_debug_read_token", "aspd_debug_bounded_wait", "aspd_debug_profile", "aspd_debug_pool_limit")
@@ -101,6 +119,7 @@ def lib() -> ctypes.CDLL:
         L.aspd_visible_slots.argtypes = [vp, vp, ci, ci, ci, vp]
         L.aspd_visible_slots_masked.argtypes = [vp, vp, ci, ci, ci, ci, vp]
         L.aspd_plan_create.argtypes = [vp, vp, vp, vp, ci, ctypes.c_int64, ci, vp, vp, vp, vp]
+        L.aspd_plan_create_scores.argtypes = [vp, vp, vp, vp, ci, ctypes.c_int64, ci, vp, vp, vp, vp, vp]
         L.aspd_plan_destroy.argtypes = [vp]
         L.aspd_plan_update.argtypes = [vp, vp, vp, vp, ci, vp, vp]
         L.aspd_release_cached_memory.argtypes = []
@@ -233,20 +252,22 @@ def visible_slots(desc, mode: int, n_slots: int, mask: int = 0) -> np.ndarray:
 
 
 class Plan:
-    """Owner of an ``aspd_plan_t`` (see ``aspd_plan_create``)."""
+    """Owner of an ``aspd_plan_t`` (see ``aspd_plan_create``; with ``scores``, a ``Scores``, ``aspd_plan_create_scores``)."""
 
     def __init__(self, shape: Shape, desc, n_pool_pages: int, mode: int, q_pos=None, kernel: int = KERNEL_AUTO,
                  chunk_tokens: int = 0, n_ctas: int = 0, host_only: bool = False, stable_cache: bool = False, stream=None,
-                 mask: int = 0, updatable: bool = False, combine: int = COMBINE_AUTO, wide_rows: int = 0, mma_m: int = 0):
+                 mask: int = 0, updatable: bool = False, combine: int = COMBINE_AUTO, wide_rows: int = 0, mma_m: int = 0,
+                 scores: Optional[Scores] = None):
         self.shape, self.mode = shape, mode
         req, br, pages = pack_descriptors(desc)
         tune = Tuning(kernel, chunk_tokens, n_ctas, 1 if host_only else 0, 1 if stable_cache else 0, mask, 1 if updatable else 0, combine, wide_rows, mma_m)
         qp = None if q_pos is None else np.ascontiguousarray(q_pos, dtype=np.int32)
         handle = ctypes.c_void_p()
         self._h = None
-        _check(lib().aspd_plan_create(ctypes.addressof(shape), _ptr(req), _ptr(br), _ptr(pages), len(req), n_pool_pages,
-                                      mode, _ptr(qp), ctypes.addressof(tune), None if host_only else _stream(stream),
-                                      ctypes.addressof(handle)), "aspd_plan_create")
+        sc = None if scores is None else scores.c_struct(shape)
+        _check(lib().aspd_plan_create_scores(ctypes.addressof(shape), _ptr(req), _ptr(br), _ptr(pages), len(req), n_pool_pages,
+                                             mode, _ptr(qp), ctypes.addressof(tune), None if sc is None else ctypes.addressof(sc),
+                                             None if host_only else _stream(stream), ctypes.addressof(handle)), "aspd_plan_create")
         self._h = handle
         self.info = PlanInfo()
         _check(lib().aspd_plan_info(self._h, ctypes.addressof(self.info)), "aspd_plan_info")

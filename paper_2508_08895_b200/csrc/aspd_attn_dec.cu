@@ -29,6 +29,7 @@
 #include <type_traits>
 
 #include "aspd_internal.cuh"
+#include "aspd_scores.cuh"
 #include "aspd_tc_common.cuh"
 
 namespace aspd {
@@ -61,6 +62,12 @@ struct DecMisc {
   int abort_flag;
 };
 
+// What the instances for plans with scores of their own keep behind it
+struct ScoreMisc {
+  int kpos[2 * kMaxSlots][16];  // position IDs of the pages' first rows (ring as nval)
+  float slope[2][64], pos[2][64];   // per query row, by item parity: slope, position ID of its token
+};
+
 struct Ctx {
   PlanDevice pd;
   const __nv_bfloat16* q;
@@ -70,7 +77,8 @@ struct Ctx {
   const char* v_pool;
   __nv_bfloat16* out;           // non-null (plans that deal whole streams): the final output; null: records for the combine kernel
   int n_q_heads, n_kv_heads, page_size;
-  float scale_log2;
+  float scale_log2;             // (1 in the instances for plans with scores of their own)
+  ScoreParams sp;               // those instances: what makes logits of the products
   int early_fetch;              // plan promise: pages without new rows are not written by in-flight work
   int k_shift, v_shift;         // log2 of the K / V tiles in flight
   uint32_t off_v, off_q, off_p, off_misc;
@@ -265,7 +273,7 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 // ---------------------------------------------------------------------------------------- softmax of an item
 // All tiles of one item: scores out of tensor memory, exponentials, P^T.  Leaves the row sums of every quadrant's
 // keys in misc->wm.
-template <int D, int NR>
+template <int D, int NR, bool SC>
 __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it, DecMisc* misc, uint32_t bars, uint32_t smem_p, uint32_t tmem,
                                              int par, int& g) {
   constexpr int HC = NR / 2;
@@ -280,6 +288,24 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
   float2 l2[HC / 2];                          // this thread's key's share of the row sums: rows r0 + 2 i, + 1
 #pragma unroll
   for (int i = 0; i < HC / 2; ++i) l2[i] = make_float2(0.f, 0.f);
+  // SC: the raw products of a tile become logits (a thread has one key and HC rows)
+  auto score = [&](float (&s)[HC], int ring, int page, int row) {
+    if constexpr (SC) {
+      const ScoreMisc* sm = reinterpret_cast<const ScoreMisc*>(misc + 1);
+      if (c.sp.cap_in != 0.f) {
+#pragma unroll
+        for (int i = 0; i < HC; ++i) s[i] = capped(s[i], c.sp);
+      } else {
+#pragma unroll
+        for (int i = 0; i < HC; ++i) s[i] *= c.sp.scale;
+      }
+      if (c.pd.slopes != nullptr) {
+        const float kp = (float)(sm->kpos[ring][page] + row);
+#pragma unroll
+        for (int i = 0; i < HC; ++i) s[i] = fmaf(sm->slope[par][r0 + i], kp - sm->pos[par][r0 + i], s[i]);
+      }
+    }
+  };
   bool settled = false, dead = false;       // settled: every row of the block has seen a key
   for (int t = 0; t < n_tiles; ++t, ++g) {
     const int sb = g & 1;
@@ -303,6 +329,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
       }
     }
     tmem_wait_ld();
+    score(s, g & (2 * kMaxSlots - 1), kl >> ps_shift, row);
     // The usual tile is one pass against the references as they are.  An exponent beyond 2^40 shows in the sum
     // and sends the tile the long way (everything is floating point: a reference up to 2^40 below a row's maximum
     // costs no precision), which an item's first tile and tiles while a row has not seen a key take anyway.
@@ -347,6 +374,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
         }
         tmem_ld<HC>(s_addr, s);
         tmem_wait_ld();
+        score(s, g & (2 * kMaxSlots - 1), kl >> ps_shift, row);
       }
       float2 tsum = make_float2(0.f, 0.f);
 #pragma unroll
@@ -366,6 +394,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
       redo = true;
       tmem_ld<HC>(s_addr, s);
       tmem_wait_ld();
+      score(s, g & (2 * kMaxSlots - 1), kl >> ps_shift, row);
     }
     tc_fence_before();
     warp_arrive(bars + 8 * (S_EMPTY + sb), lane);                 // the scores are not needed again
@@ -452,7 +481,7 @@ __device__ __forceinline__ bool finish_item(const Ctx& c, const DeviceItem& it, 
 // tuned, since finite values never come here (a vote that the item's end takes anyway asks for it) and a function
 // of its own keeps it out of the loop's code.  What the steps pay for asking, us a layer before and now: 8 requests with
 // heads of 64 from the host 14.6 and 14.8, steps with pages of 8 or 32 up to 2 % (inlined: up to 3 %).
-template <int D>
+template <int D, bool SC>
 __device__ __noinline__ void redo_item(const Ctx& c, const DeviceItem it, DecMisc* misc, float* q_sm, int par) {
   constexpr int EPL = D / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = c.n_q_heads / c.n_kv_heads, M = it.n_q_tok * G;
@@ -473,6 +502,8 @@ __device__ __noinline__ void redo_item(const Ctx& c, const DeviceItem it, DecMis
     }
     __syncwarp();
     const int4 vis = misc->vis[par][r / G];
+    RowBias rb = {0.f, 0};
+    if (SC && c.pd.slopes != nullptr) rb = row_bias(c.pd, tok, it.kv_head * G + r % G);
     float m = -INFINITY, l = 0.f, acc[EPL];
 #pragma unroll
     for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
@@ -496,6 +527,10 @@ __device__ __noinline__ void redo_item(const Ctx& c, const DeviceItem it, DecMis
             const float2 x = __bfloat1622float2(k2[i]), w = *reinterpret_cast<const float2*>(qw + ch * 8 + 2 * i);
             s = fmaf(w.x, x.x, s); s = fmaf(w.y, x.y, s);
           }
+        }
+        if constexpr (SC) {
+          s = c.sp.cap_in != 0.f ? capped(s, c.sp) : s * c.sp.scale;
+          if (c.pd.slopes != nullptr) s = fmaf(rb.slope, (float)(c.pd.page_pos[it.page0 + j / ps] + row - rb.pos), s);
         }
       }
       float mn = s;
@@ -537,7 +572,7 @@ __device__ __noinline__ void redo_item(const Ctx& c, const DeviceItem it, DecMis
 // NR: rows that the plan's largest row block is padded to; its smaller blocks are padded as far.  (One instance that
 // chose per item was 161 KB of code, these are 65 to 99, and a short launch waits for its instructions: 14.5 against
 // 14.1 us a layer in a graph on the step above.)
-template <int D, int NR>
+template <int D, int NR, bool SC>
 __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_constant__ Ctx c) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -552,6 +587,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
   const int ps = c.page_size, ps_shift = 31 - __clz(ps), ppt = kTile >> ps_shift;
   int2 first_pages = make_int2(0, 0);
   if ((warp == W_K || warp == W_V) && lane < head.w) first_pages = c.pd.visit[head.z + lane];
+  ScoreMisc* const sm = reinterpret_cast<ScoreMisc*>(misc + 1);
+  const bool page_positions = SC && warp == W_K && c.pd.page_pos != nullptr;
+  int first_pos = 0;
+  if (page_positions && lane < head.w) first_pos = c.pd.page_pos[head.z + lane];
   if (tid == 0) {
     auto count = [](int i) { return i >= S_EMPTY && i < P_FULL ? 8 : i == P_FULL || i == Q_FULL ? 8 : i == A_DONE ? 2 : 1; };   // one arrival per warp that takes part
     for (int i = 0; i < NUM_BARS; ++i) mbar_init(bars + 8 * i, count(i));
@@ -591,7 +630,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
         row_out = c.out != nullptr ? tok * c.n_q_heads + it.kv_head * G + tid % G
                                    : (c.pd.part_base[tok * c.n_kv_heads + it.kv_head] + it.part_slot) * G + tid % G;
       }
+      RowBias rb = {0.f, 0};
+      if (SC && c.pd.slopes != nullptr && tid < m) rb = row_bias(c.pd, it.q_tok0 + tid / G, it.kv_head * G + tid % G);
       prep_q<D, NR>(c, it, base + c.off_q, tid);
+      if constexpr (SC) {
+        if (tid < NR) { sm->slope[par][tid] = rb.slope; sm->pos[par][tid] = (float)rb.pos; }
+      }
       if (tid < it.n_q_tok) misc->vis[par][tid] = vis;
       if (tid < m) misc->row_out[par][tid] = row_out;
       warp_arrive(bars + 8 * Q_FULL, lane);
@@ -601,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
       const DeviceItem it = idx == item_begin ? first : uniform_item(c.pd.items[idx]);
       const int par = item_no & 1;
       named_sync(1, kSmThreads);                                  // the item's ranges are there
-      dead |= !softmax_item<D, NR>(c, it, misc, bars, base + c.off_p, tmem, par, g);
+      dead |= !softmax_item<D, NR, SC>(c, it, misc, bars, base + c.off_p, tmem, par, g);
       if (idx + 1 < item_end) {                                   // the next query tile as soon as this item's last scores are issued
         dead |= !mbar_wait(bars + 8 * Q_EMPTY, item_no & 1, ab);
         start_item(uniform_item(c.pd.items[idx + 1]), par ^ 1);
@@ -614,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
       if (named_sync_or(1, kSmThreads, bad || dead || *ab)) {
         if (c.k_new != nullptr) dead |= !mbar_wait(bars + 8 * A_DONE, 0, ab);     // the step's own rows are in the pools
         if (named_sync_or(1, kSmThreads, dead || *ab)) break;
-        redo_item<D>(c, it, misc, reinterpret_cast<float*>(smem_raw + (base - raw) + c.off_p), par);
+        redo_item<D, SC>(c, it, misc, reinterpret_cast<float*>(smem_raw + (base - raw) + c.off_p), par);
       }
     }
   } else if (producer) {
@@ -629,20 +673,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
     int g = 0;
     bool ok = true, appended = false, waited = false;
     int2 nxt = first_pages;
+    int nxt_pos = first_pos;
     for (int idx = item_begin; idx < item_end && ok; ++idx) {
       const DeviceItem it = uniform_item(c.pd.items[idx]);
       const int n_tiles = (it.n_pages + ppt - 1) / ppt;
       int2 cur = make_int2(0, 0);
+      int cur_pos = 0;
       for (int t = 0; t < n_tiles && ok; ++t, ++g) {
         if (t % tpb == 0) {
           cur = nxt;
           nxt = make_int2(0, 0);
+          if constexpr (SC) { cur_pos = nxt_pos; nxt_pos = 0; }
           const int ahead = (t + tpb) * ppt;
           if (ahead < it.n_pages) {
             if (ahead + lane < it.n_pages) nxt = c.pd.visit[it.page0 + ahead + lane];
+            if (page_positions && ahead + lane < it.n_pages) nxt_pos = c.pd.page_pos[it.page0 + ahead + lane];
           } else if (idx + 1 < item_end) {
             const int2 nx = make_int2(c.pd.items[idx + 1].page0, c.pd.items[idx + 1].n_pages);
             if (lane < nx.y) nxt = c.pd.visit[nx.x + lane];
+            if (page_positions && lane < nx.y) nxt_pos = c.pd.page_pos[nx.x + lane];
           }
         }
         const int npg = min(ppt, it.n_pages - t * ppt);
@@ -668,6 +717,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
         ok = __all_sync(0xffffffffu, mbar_wait(empty, (fill & 1) ^ 1, ab)) != 0;
         if (!ok) break;
         if (!is_v && lane < 16) misc->nval[g & (2 * kMaxSlots - 1)][lane] = pg.y;   // read by the softmax warps of tile g
+        if constexpr (SC) {
+          const int kp = __shfl_sync(0xffffffffu, cur_pos, src_lane);
+          if (page_positions && lane < 16) sm->kpos[g & (2 * kMaxSlots - 1)][lane] = kp;
+        }
         __syncwarp();
         if (lane == 0) mbar_expect_tx(full, (uint32_t)ncopy * page_bytes);
         __syncwarp();
@@ -747,9 +800,10 @@ inline uint32_t up1k(uint32_t x) { return (x + 1023u) & ~1023u; }
 
 // Shared memory of a plan whose row blocks are padded to nr rows: 1 to 4 K tiles and V tiles, as many as fit.
 constexpr uint32_t kSmemMax = 232448;
-inline uint32_t smem_layout(int D, int nr, Ctx* c) {
+inline uint32_t smem_layout(int D, int nr, bool scored, Ctx* c) {
+  const uint32_t misc = (uint32_t)(sizeof(DecMisc) + (scored ? sizeof(ScoreMisc) : 0));
   const uint32_t tile = kTile * D * 2, q = up1k(kPieces * nr * D * 2), p = up1k(kPieces * kTile * nr * 2);
-  const uint32_t rest = q + p + (uint32_t)sizeof(DecMisc) + 1024;       // + slack to align the base
+  const uint32_t rest = q + p + misc + 1024;       // + slack to align the base
   auto fits = [&](int k, int v) { return ((1u << k) + (1u << v)) * tile + rest <= kSmemMax; };
   c->k_shift = fits(2, 2) ? 2 : fits(1, 0) ? 1 : 0;
   c->v_shift = fits(2, 2) ? 2 : fits(1, 1) ? 1 : 0;
@@ -757,22 +811,26 @@ inline uint32_t smem_layout(int D, int nr, Ctx* c) {
   c->off_q = c->off_v + (tile << c->v_shift);
   c->off_p = c->off_q + q;
   c->off_misc = c->off_p + p;
-  return c->off_misc + (uint32_t)sizeof(DecMisc) + 1024;
+  return c->off_misc + misc + 1024;
 }
 
-template <int D, int NR>
-cudaError_t launch(const aspd_plan* p, Ctx& c, cudaStream_t s) {
+template <int D, int NR, bool SC>
+cudaError_t launch_instance(const aspd_plan* p, Ctx& c, cudaStream_t s) {
   static bool configured[64] = {};                 // the attribute belongs to the (function, device) pair
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(attn_dec_kernel<D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
+    e = cudaFuncSetAttribute(attn_dec_kernel<D, NR, SC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  const uint32_t smem = smem_layout(D, NR, &c);
-  return launch_pdl(attn_dec_kernel<D, NR>, dim3(p->n_ctas), dim3(kThreads), smem, s, c);
+  const uint32_t smem = smem_layout(D, NR, SC, &c);
+  return launch_pdl(attn_dec_kernel<D, NR, SC>, dim3(p->n_ctas), dim3(kThreads), smem, s, c);
+}
+template <int D, int NR>
+cudaError_t launch(const aspd_plan* p, Ctx& c, cudaStream_t s) {
+  return p->scored() ? launch_instance<D, NR, true>(p, c, s) : launch_instance<D, NR, false>(p, c, s);
 }
 
 }  // namespace
@@ -788,7 +846,8 @@ int launch_attn_dec(const aspd_plan* p, const void* q, const void* k_new, const 
   c.k_pool = (const char*)k_pool; c.v_pool = (const char*)v_pool;
   c.out = p->dealt ? (__nv_bfloat16*)out : nullptr;
   c.n_q_heads = sh.n_q_heads; c.n_kv_heads = sh.n_kv_heads; c.page_size = sh.page_size;
-  c.scale_log2 = sh.sm_scale * kLog2e;
+  c.scale_log2 = p->scored() ? 1.f : sh.sm_scale * kLog2e;
+  c.sp = score_params(p);
   c.early_fetch = p->stable_cache;
   const int nr = padded_rows(p->max_rows);
   const cudaError_t e = sh.head_dim == 64 ? (nr == 16 ? launch<64, 16>(p, c, s) : nr == 32 ? launch<64, 32>(p, c, s) : launch<64, 64>(p, c, s))

@@ -29,6 +29,7 @@
 
 #include "aspd_internal.cuh"
 #include "aspd_combine.cuh"
+#include "aspd_scores.cuh"
 #include "aspd_tc_common.cuh"
 
 namespace aspd {
@@ -75,6 +76,7 @@ struct Misc {
   int abort_flag;
   int mq_n;                    // merge queue (plans that merge inside the kernel): filled by the epilogue warps with
   int mq[kMergeQueue][3];      // (token * n_kv_heads + KV head, first record, number of records)
+  int kpos[4][8];              // plans with a distance bias: position ID of the first row of the 8 pages of a tile (ring as nval)
 };
 static_assert(sizeof(Misc) <= 8192, "Misc must fit into the unused rows of the P tile");
 // The step's new rows (512 bytes each: K, rotated, and V) wait in shared memory until their tiles have landed (plans
@@ -110,7 +112,8 @@ struct Ctx {
   const char* v_pool;
   int n_items, n_q_heads, n_kv_heads;
   int G, inv_g;                // query heads of a KV head; 65536 / G rounded up (token_of)
-  float scale_log2;
+  float scale_log2;            // (1 in the instances for plans with scores of their own)
+  ScoreParams sp;              // those instances: what makes logits of the products
   int early_fetch;             // plan promise: pages without new rows are not written by in-flight work
   int m64;                     // MMAs with M = 64: row blocks of at most 64 rows are not padded to 128 (half the tensor work)
   int pv64;                    // only P.V with M = 64 (scores and the softmax layout stay at M = 128): O then sits in 16 lanes
@@ -149,7 +152,8 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
   return hi > lo ? ((0xFFFFu >> (16 - hi)) & ~((1u << lo) - 1u)) : 0u;
 }
 
-template <int NC>   // NC = padded row count R = columns of a row replica; a thread takes half of them
+// SC: the plan's scores are capped or have a distance bias (score_row)
+template <int NC, bool SC>   // NC = padded row count R = columns of a row replica; a thread takes half of them
 __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p,
                                              uint32_t tmem, int item_no, int& g) {   // item_no = index among this CTA's items
   constexpr int R = NC, KS = 128 / NC, HC = NC / 2;
@@ -163,6 +167,9 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
   int4 vis = make_int4(0, 0, 0, 0);             // padding rows see nothing
   const int tl = token_of(c, r);
   if (r < M) vis = (item_no < kItemCache && tl < kMaxTokPerItem) ? misc->vis[item_no][tl] : c.pd.tok_vis[it.q_tok0 + tl];
+  RowBias rb = {0.f, 0};
+  const bool biased = SC && c.pd.slopes != nullptr;
+  if (biased && r < M) rb = row_bias(c.pd, it.q_tok0 + tl, it.kv_head * G + r - tl * G);
   const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
   const bool o_owner = half == 0 && (warp & 3) < R / 32;   // threads whose TMEM lane holds a row of O
   const int ob = item_no & 1;
@@ -179,6 +186,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
     if constexpr (HC == 32) ASPD_TMEM_LD32(s_addr, s, 0);
     else ASPD_TMEM_LD16(s_addr, s, 0);
     tmem_wait_ld();
+    if constexpr (SC) score_row(s, c.sp, biased, rb, &misc->kpos[g & 3][col0 / 16]);
     if (tid == 0) ASPD_STAMP(c, g, 1);
     // After an item's first tile the rows have a reference maximum, and a tile's exponentials are taken against it right
     // away: one pass (mask, packed fp32 pairs, the exponentials), no maximum, no exchange between the threads of a row.
@@ -221,6 +229,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
         if constexpr (HC == 32) ASPD_TMEM_LD32(s_addr, s, 0);
         else ASPD_TMEM_LD16(s_addr, s, 0);
         tmem_wait_ld();
+        if constexpr (SC) score_row(s, c.sp, biased, rb, &misc->kpos[g & 3][col0 / 16]);
       }
     }
     if (tid == 0) ASPD_STAMP(c, g, 2);
@@ -524,6 +533,7 @@ __device__ __forceinline__ bool softmax_item_m64(const Ctx& c, const DeviceItem&
 // tile: the exponentials are taken against the current reference maximum while the largest
 // exponent is tracked; only when a row's largest exponent exceeds 2^8 (always on the row's first
 // visible key) the reference is raised and the warp repeats the pass from TMEM.
+template <bool SC>
 __device__ __forceinline__ bool softmax_item_wide(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p,
                                                   uint32_t tmem, int item_no, int& g) {
   const int tid = threadIdx.x, warp = uniform(tid >> 5);
@@ -536,6 +546,9 @@ __device__ __forceinline__ bool softmax_item_wide(const Ctx& c, const DeviceItem
   int4 vis = make_int4(0, 0, 0, 0);
   const int tl = token_of(c, r);
   if (r < M) vis = (item_no < kItemCache && tl < kMaxTokPerItem) ? misc->vis[item_no][tl] : c.pd.tok_vis[it.q_tok0 + tl];
+  RowBias rb = {0.f, 0};
+  const bool biased = SC && c.pd.slopes != nullptr;
+  if (biased && r < M) rb = row_bias(c.pd, it.q_tok0 + tl, it.kv_head * G + r - tl * G);
   const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
   const bool o_owner = half == 0;
   const int ob = item_no & 1;
@@ -562,6 +575,7 @@ __device__ __forceinline__ bool softmax_item_wide(const Ctx& c, const DeviceItem
         float s[32];
         ASPD_TMEM_LD32(s_addr + ch * 32, s, 0);
         tmem_wait_ld();
+        if constexpr (SC) score_row(s, c.sp, biased, rb, &misc->kpos[g & 3][col0 / 16 + ch * 2]);
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
           const int ye = misc->nval[g & 3][col0 / 16 + ch * 2 + pg], nv = ye & 255;
@@ -812,7 +826,8 @@ __device__ __forceinline__ bool patch_tile(uint32_t base, uint32_t bars, volatil
 //              narrow row blocks
 //   kPatch     kPlain for fused steps of plans that patch their tiles (patch_tile)
 enum { kPlain = 0, kOptions = 1, kPatch = 2 };
-template <bool WIDE, int MODE>
+// SC: instances for plans whose scores are not the plain products.
+template <bool WIDE, int MODE, bool SC>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
   constexpr bool OPT = MODE == kOptions, PATCH = MODE == kPatch;
   extern __shared__ uint8_t smem_raw[];
@@ -847,6 +862,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
   // is the second load of the kernel, not the fourth) are fetched while the CTA is still setting up.
   int2 first_pages = make_int2(0, 0);
   if ((warp == W_KPROD || warp == W_VPROD) && lane < head.w) first_pages = c.pd.visit[head.z + lane];
+  const bool page_positions = SC && warp == W_KPROD && c.pd.page_pos != nullptr;
+  int first_pos = 0;
+  if (page_positions && lane < head.w) first_pos = c.pd.page_pos[head.z + lane];
   // fused step: the CTA's new rows (plan data), an entry per lane of the warps that deal with them
   // (PATCH: the planner lists at most kMostFusedRows of a CTA for such launches; no more than that ever has a place)
   const int dirty_rows = c.k_new == nullptr ? 0 : uniform(PATCH ? min(head2.y, kMostFusedRows) : head2.y);
@@ -897,16 +915,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const int M = it.n_q_tok * c.G;
       bool ok;
       if constexpr (WIDE) {
-        ok = M <= 32 ? softmax_item<32>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-           : M <= 64 ? softmax_item<64>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-                     : softmax_item_wide(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
+        ok = M <= 32 ? softmax_item<32, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
+           : M <= 64 ? softmax_item<64, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
+                     : softmax_item_wide<SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
       } else {
-        if (OPT && c.m64)
-          ok = M <= 32 ? softmax_item_m64<32>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-                       : softmax_item_m64<64>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
-        else
-          ok = M <= 32 ? softmax_item<32>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-                       : softmax_item<64>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
+        bool scores64 = false;                     // scores with M = 64 (plans with scores of their own never have them)
+        if constexpr (OPT && !SC) {
+          scores64 = c.m64;
+          if (scores64)
+            ok = M <= 32 ? softmax_item_m64<32>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
+                         : softmax_item_m64<64>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
+        }
+        if (!scores64)
+          ok = M <= 32 ? softmax_item<32, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
+                       : softmax_item<64, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
       }
       if (!ok) break;
     }
@@ -924,20 +946,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
     // (item, batch of 32 pages) pairs are walked as one sequence: `cur` holds the batch being
     // consumed, `nxt` the one after it, which may already belong to the next item.
     int2 nxt = first_pages;
+    int nxt_pos = first_pos;
     for (int idx = item_begin; idx < item_end && ok; ++idx) {
       const DeviceItem it = get_item(c, misc, idx, item_begin);
       const int n_tiles = (it.n_pages + 7) >> 3;
       int2 cur = make_int2(0, 0);
+      int cur_pos = 0;
       for (int t = 0; t < n_tiles && ok; ++t, ++g) {
         if ((t & 3) == 0) {
           cur = nxt;
           nxt = make_int2(0, 0);
+          if constexpr (SC) { cur_pos = nxt_pos; nxt_pos = 0; }
           const int ahead = (t + 4) * 8 + lane;
           if ((t + 4) * 8 < it.n_pages) {
             if (ahead < it.n_pages) nxt = c.pd.visit[it.page0 + ahead];
+            if (page_positions && ahead < it.n_pages) nxt_pos = c.pd.page_pos[it.page0 + ahead];
           } else if (idx + 1 < item_end) {          // first batch of the next item
             const DeviceItem nx = get_item(c, misc, idx + 1, item_begin);
             if (lane < nx.n_pages) nxt = c.pd.visit[nx.page0 + lane];
+            if (page_positions && lane < nx.n_pages) nxt_pos = c.pd.page_pos[nx.page0 + lane];
           }
         }
         const int npg = min(8, it.n_pages - t * 8), sl = g & 1;
@@ -973,6 +1000,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
           __syncwarp();
         }
         if (kv == 0 && lane < 8) misc->nval[g & 3][lane] = pg.y;   // read by the softmax warps of tile g
+        if constexpr (SC) {
+          const int kp = __shfl_sync(0xffffffffu, cur_pos, (t & 3) * 8 + (lane & 7));
+          if (page_positions && lane < 8) misc->kpos[g & 3][lane] = kp;
+        }
         __syncwarp();
         if (lane == 0) mbar_expect_tx(full, (uint32_t)npg * 4096u);
         __syncwarp();
@@ -1290,9 +1321,12 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
     auto attr = [](auto* kernel, size_t bytes) {
       return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
     };
-    if (!attr(attn_tc_kernel<false, kPlain>, kSmemBytes) || !attr(attn_tc_kernel<false, kOptions>, kSmemBytes) ||
-        !attr(attn_tc_kernel<false, kPatch>, kSmemBytes) || !attr(attn_tc_kernel<true, kPlain>, kSmemBytes) || !attr(attn_tc_w2_kernel, kSmemBytesW2))
-      return ASPD_ERR_CUDA;
+    auto all = [&](auto sc) {
+      constexpr bool SC = decltype(sc)::value;
+      return attr(attn_tc_kernel<false, kPlain, SC>, kSmemBytes) && attr(attn_tc_kernel<false, kOptions, SC>, kSmemBytes) &&
+             attr(attn_tc_kernel<false, kPatch, SC>, kSmemBytes) && attr(attn_tc_kernel<true, kPlain, SC>, kSmemBytes) && attr(attn_tc_w2_kernel<SC>, kSmemBytesW2);
+    };
+    if (!all(std::false_type()) || !all(std::true_type())) return ASPD_ERR_CUDA;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   Ctx c;
@@ -1313,7 +1347,8 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
   c.n_kv_heads = sh.n_kv_heads;
   c.G = sh.n_q_heads / sh.n_kv_heads;
   c.inv_g = (65536 + c.G - 1) / c.G;
-  c.scale_log2 = sh.sm_scale * kLog2e;
+  c.scale_log2 = p->scored() ? 1.f : sh.sm_scale * kLog2e;
+  c.sp = score_params(p);
   c.early_fetch = p->stable_cache;
   c.stagger_start = p->stagger_start;
   c.m64 = (p->m64 == 1 && !p->wide && !p->dealt) ? 1 : 0;
@@ -1323,11 +1358,16 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
   if (p->wide == 2) {                       // row blocks of two query tiles: final outputs only
     if (c.out == nullptr) return ASPD_ERR_UNSUPPORTED;
     c.k_new = nullptr; c.v_new = nullptr;
-    return launch_pdl(attn_tc_w2_kernel, dim3(p->n_ctas), dim3(kThreadsW2), kSmemBytesW2, s, c) == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
+    return launch_pdl(p->scored() ? attn_tc_w2_kernel<true> : attn_tc_w2_kernel<false>, dim3(p->n_ctas), dim3(kThreadsW2), kSmemBytesW2, s, c) == cudaSuccess
+               ? ASPD_OK : ASPD_ERR_CUDA;
   }
-  auto* kernel = p->wide ? attn_tc_kernel<true, kPlain>
-                 : c.m64 || c.merge_out != nullptr || c.out != nullptr ? attn_tc_kernel<false, kOptions>
-                 : c.k_new != nullptr && p->patch_tiles ? attn_tc_kernel<false, kPatch> : attn_tc_kernel<false, kPlain>;
+  auto instance = [&](auto sc) {
+    constexpr bool SC = decltype(sc)::value;
+    return p->wide ? attn_tc_kernel<true, kPlain, SC>
+           : c.m64 || c.merge_out != nullptr || c.out != nullptr ? attn_tc_kernel<false, kOptions, SC>
+           : c.k_new != nullptr && p->patch_tiles ? attn_tc_kernel<false, kPatch, SC> : attn_tc_kernel<false, kPlain, SC>;
+  };
+  auto* kernel = p->scored() ? instance(std::true_type()) : instance(std::false_type());
   const cudaError_t e = launch_pdl(kernel, dim3(p->n_ctas), dim3(kThreads), kSmemBytes, s, c);
   return e == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
 }

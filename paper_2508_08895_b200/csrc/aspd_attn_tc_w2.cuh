@@ -56,6 +56,7 @@ struct MiscW2 {
   uint32_t tmem_base;
   int abort_flag;
   int lead;                          // the item group 0's issuer is at (read by group 1's)
+  int kpos[kPageRingW2][8];          // plans with a distance bias: position IDs of the pages' first rows (ring as nval)
 };
 static_assert(sizeof(MiscW2) <= 2048, "MiscW2 must fit behind the tiles");
 
@@ -110,6 +111,7 @@ __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok
 }
 
 // One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.
+template <bool SC>
 __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                  int item_end, int grp, int tpt) {
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, r = tid & 127;
@@ -143,6 +145,9 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
     const int tl = token_of(c, r), M = n_tok * G, tok = it.q_tok0 + grp * tpt + tl;
     int4 vis = make_int4(0, 0, 0, 0);                          // padding rows see nothing
     if (r < M) vis = c.pd.tok_vis[tok];
+    RowBias rb = {0.f, 0};
+    const bool biased = SC && c.pd.slopes != nullptr;
+    if (biased && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
     float m_ref = 0.f, l = 0.f;                                 // see the one-tile variant: the reference starts at 0
     bool seen = r >= M;                                         // padding rows never need the tracking pass
     bool warp_seen = false;                                     // all rows of the warp have (kept up in the full path only)
@@ -189,7 +194,8 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 #pragma unroll
           for (int ch = 0; ch < 2; ++ch) {
             if (ch == 1) tmem_wait_ld32(s1);
-            const float (&s)[32] = ch ? s1 : s0;
+            float (&s)[32] = ch ? s1 : s0;
+            if constexpr (SC) score_row(s, c.sp, biased, rb, &misc->kpos[g & (kPageRingW2 - 1)][4 * h + 2 * ch]);
 #pragma unroll
             for (int pg = 0; pg < 2; ++pg) {
               const int nv = (h ? ye8[4 + ch * 2 + pg] : ye8[ch * 2 + pg]) & 255;
@@ -316,6 +322,7 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 }
 
 
+template <bool SC>
 __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -331,6 +338,9 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   const int item_begin = uniform(head.x), item_end = uniform(head.y);
   int2 first_pages = make_int2(0, 0);
   if ((warp == W2_KPROD || warp == W2_VPROD) && lane < head.w) first_pages = c.pd.visit[head.z + lane];
+  const bool page_positions = SC && warp == W2_KPROD && c.pd.page_pos != nullptr;
+  int first_pos = 0;
+  if (page_positions && lane < head.w) first_pos = c.pd.page_pos[head.z + lane];
   {
     const int n_cached = min(item_end - item_begin, kItemCacheW2);
     for (int e = tid; e < n_cached * (int)(sizeof(DeviceItem) / 4); e += kThreadsW2)
@@ -362,7 +372,7 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   if (tid == 0) ASPD_CTA_STAMP(c, 1);
 
   if (warp < 8) {
-    softmax_group_w2(c, misc, bars, base, tmem, item_begin, item_end, warp >> 2, tpt);
+    softmax_group_w2<SC>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 2, tpt);
   } else if (warp == W2_KPROD || warp == W2_VPROD) {
     // ================================ bulk-copy producers (as in the other variants) ================================
     const int kv = warp == W2_KPROD ? 0 : 1;
@@ -370,20 +380,25 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
     int g = 0;
     bool ok = true, waited = false;
     int2 nxt = first_pages;
+    int nxt_pos = first_pos;
     for (int idx = item_begin; idx < item_end && ok; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
       const int n_tiles = (it.n_pages + 7) >> 3;
       int2 cur = make_int2(0, 0);
+      int cur_pos = 0;
       for (int t = 0; t < n_tiles && ok; ++t, ++g) {
         if ((t & 3) == 0) {
           cur = nxt;
           nxt = make_int2(0, 0);
+          if constexpr (SC) { cur_pos = nxt_pos; nxt_pos = 0; }
           const int ahead = (t + 4) * 8 + lane;
           if ((t + 4) * 8 < it.n_pages) {
             if (ahead < it.n_pages) nxt = c.pd.visit[it.page0 + ahead];
+            if (page_positions && ahead < it.n_pages) nxt_pos = c.pd.page_pos[it.page0 + ahead];
           } else if (idx + 1 < item_end) {          // first batch of the next item
             const DeviceItem nx = get_item_w2(c, misc, idx + 1, item_begin);
             if (lane < nx.n_pages) nxt = c.pd.visit[nx.page0 + lane];
+            if (page_positions && lane < nx.n_pages) nxt_pos = c.pd.page_pos[nx.page0 + lane];
           }
         }
         const int npg = min(8, it.n_pages - t * 8), sl = g & 1;
@@ -403,6 +418,10 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
         if (!good) { ok = false; break; }
         if (lane == 0) ASPD_STAMP(c, g, 13 + kv);
         if (kv == 0 && lane < 8) misc->nval[g & (kPageRingW2 - 1)][lane] = pg.y;   // read by the softmax groups of tile g
+        if constexpr (SC) {
+          const int kp = __shfl_sync(0xffffffffu, cur_pos, (t & 3) * 8 + (lane & 7));
+          if (page_positions && lane < 8) misc->kpos[g & (kPageRingW2 - 1)][lane] = kp;
+        }
         __syncwarp();
         if (lane == 0) mbar_expect_tx(full, (uint32_t)npg * 4096u);
         __syncwarp();

@@ -63,6 +63,10 @@ struct PlanDevice {       // pointers into the plan's single device allocation
   int32_t* work_counter;       // dynamic work-list cursor (reset by its last reader)
   int32_t* arrive;             // [n_new * n_kv_heads] records of (new token, KV head) stored so far in this launch (plans
                                // that merge inside the attention kernel; zero between launches)
+  // plans with a distance bias (null otherwise)
+  const int32_t* page_pos;     // per entry of `visit`: position ID of the page's first row
+  const int32_t* bias_pos;     // [n_new] position ID of the new token (tok_pos may be the caller's, or all 0)
+  const float* slopes;         // [n_q_heads] in log2 units
   // staging for aspd_step_host
   void* st_q; void* st_k; void* st_v; void* st_out; int32_t* st_pos;
   int32_t pool_limit;          // pages in each pool: what builds with -DASPD_DEBUG_BOUNDS check page ids against
@@ -89,7 +93,7 @@ namespace aspd {
 // length-dependent ones have room for.
 struct PlanLayout {
   size_t o_items = 0, o_cta = 0, o_visit = 0, o_dirty = 0, o_tpage = 0, o_trow = 0, o_tpos = 0, o_tvis = 0,
-         o_rb = 0, o_pbase = 0, o_freq = 0, o_status = 0, o_arrive = 0, upload_bytes = 0, cleared_end = 0, o_qcs = 0, o_wso = 0, o_wsml = 0, o_stq = 0,
+         o_rb = 0, o_pbase = 0, o_freq = 0, o_ppos = 0, o_bpos = 0, o_slope = 0, o_status = 0, o_arrive = 0, upload_bytes = 0, cleared_end = 0, o_qcs = 0, o_wso = 0, o_wsml = 0, o_stq = 0,
          o_stk = 0, o_stv = 0, o_sto = 0, o_stp = 0, device_bytes = 0;
   size_t cap_items = 0, cap_visit = 0, cap_dirty = 0, cap_partials = 0, n_row_blocks = 0, n_part_base = 0;
 };
@@ -134,6 +138,11 @@ struct aspd_plan {
   int stagger_start = 0;           // few tiles per CTA: order the requests of a CTA's first tiles (see the producers)
   int patch_tiles = 0;             // at most two tiles per CTA on average: a fused step puts the new rows into the tiles (see patch_tile)
   int single_launch = 0;           // stream-K plan of the tensor-core kernel whose last-arriving CTAs merge the records themselves
+  float cap = 0.f;                 // scores are capped (0: not)
+  int rotated = 0;                 // q and k_new come rotated
+  std::vector<float> slopes;       // distance bias per query head (empty: none)
+  std::vector<int32_t> page_pos, bias_pos;   // with slopes: see PlanDevice
+  bool scored() const { return cap > 0.f || !slopes.empty(); }   // the scores are not the plain products
   int64_t n_pool_pages = 0;
   int64_t kv_tokens_read = 0;
   int64_t algorithmic_bytes = 0;
@@ -225,6 +234,10 @@ inline void fill_cta_head(const aspd_plan* p, int4* dst) {
     dst[2 * c] = make_int4(b, e, b < e ? p->items[b].page0 : 0, b < e ? p->items[b].n_pages : 0);
     dst[2 * c + 1] = make_int4(p->cta_dirty0[c], p->cta_dirty0[c + 1] - p->cta_dirty0[c], 0, 0);
   }
+}
+// the device plan's slopes, from the host's
+inline void fill_slopes(const aspd_plan* p, float* dst) {
+  for (size_t h = 0; h < p->slopes.size(); ++h) dst[h] = p->slopes[h] * 1.4426950408889634f;
 }
 inline int esize_of(int dtype) { return dtype == ASPD_DTYPE_BF16 ? 2 : 4; }
 // device buffers are moved in 16-byte pieces: a pointer off that boundary is refused, not dereferenced

@@ -2,6 +2,7 @@
 // supported dtype / head_dim / page_size), the log-sum-exp combine (a7) and a debug reader.
 #include "aspd_internal.cuh"
 #include "aspd_combine.cuh"
+#include "aspd_scores.cuh"
 
 namespace aspd {
 
@@ -294,10 +295,12 @@ __device__ __forceinline__ void lane_elems(const T* tile, int tok, int lane, flo
   for (int i = 0; i < D / 32; ++i) x[i] = to_f32(e[i]);
 }
 
-template <typename T, int D, int RPW>
+// SC: scores of their own.  scale then only takes the products to natural logits, and the cap is CUDA's tanhf (fp32 outputs
+// see a logit's absolute error of 2^-22 of the cap, which the tensor-core kernels' form has).
+template <typename T, int D, int RPW, bool SC>
 __device__ __forceinline__ void generic_item(const PlanDevice& pd, const DeviceItem& it, GenSmem<T, D>& sm, const T* __restrict__ q,
                                              const T* __restrict__ k_pool, const T* __restrict__ v_pool, int n_q_heads, int n_kv_heads,
-                                             int page_size, float scale_log2) {
+                                             int page_size, float scale_log2, float cap) {
   constexpr int EPL = D / 32, EPC = 16 / (int)sizeof(T), RB = D * (int)sizeof(T);
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int G = n_q_heads / n_kv_heads, n_rows = it.n_q_tok * G, ppc = kGenKeys / page_size;   // pages of a chunk (4, 2, 1)
@@ -338,6 +341,18 @@ __device__ __forceinline__ void generic_item(const PlanDevice& pd, const DeviceI
     sm.q[r * D + i + D / 2] = (x1 * cs.x + x0 * cs.y) * scale_log2;
   }
   const int row0 = warp * RPW;                    // rows row0 ... row0 + RPW - 1, those below n_rows
+  RowBias rb[SC ? RPW : 1];
+  auto pos_of = [&](int chunk) {                  // as entry_of: position ID of the first row of page l
+    return SC && pd.page_pos != nullptr && lane < ppc && chunk * ppc + lane < it.n_pages ? pd.page_pos[it.page0 + chunk * ppc + lane] : 0;
+  };
+  int cur_pos = pos_of(0), nxt_pos = pos_of(1);
+  if constexpr (SC) {
+#pragma unroll
+    for (int i = 0; i < RPW; ++i) {
+      const int r = min(row0 + i, n_rows - 1);
+      rb[i] = row_bias(pd, it.q_tok0 + r / G, it.kv_head * G + r % G);
+    }
+  }
   float m[RPW], l[RPW], acc[RPW][EPL];
 #pragma unroll
   for (int i = 0; i < RPW; ++i) {
@@ -348,6 +363,7 @@ __device__ __forceinline__ void generic_item(const PlanDevice& pd, const DeviceI
   for (int ch = 0; ch < n_chunks; ++ch) {
     const int st = ch & 1;
     const int2 after = entry_of(ch + 2);
+    const int after_pos = pos_of(ch + 2);
     if (ch + 1 < n_chunks) { request(nxt, st ^ 1); cp_async_wait<1>(); }
     else cp_async_wait<0>();
     __syncthreads();
@@ -377,11 +393,17 @@ __device__ __forceinline__ void generic_item(const PlanDevice& pd, const DeviceI
       // branches whose offset in their branch (page index in the upper bits of the page entry) is below w
       const int ye = __shfl_sync(0xffffffffu, cur.y, lane >> page_shift), row = lane & (page_size - 1), kg = it.key0 + ch * kGenKeys + lane;
       const bool valid = row < (ye & 255);
+      const int kp = SC ? __shfl_sync(0xffffffffu, cur_pos, lane >> page_shift) + row : 0;
 #pragma unroll
       for (int i = 0; i < RPW; ++i) {
         const int4 vis = sm.vis[min(row0 + i, n_rows - 1) / G];
         const bool seen = valid && (kg < vis.x || (kg >= vis.y && kg < vis.z) || (ye >> 13) * page_size + row < vis.w);
-        const float x = seen ? s[i][0] + s[i][1] : -INFINITY;
+        float logit = s[i][0] + s[i][1];
+        if constexpr (SC) {
+          if (cap > 0.f) logit = cap * tanhf(logit / cap);
+          logit = fmaf(rb[i].slope, (float)(kp - rb[i].pos), logit * kLog2e);
+        }
+        const float x = seen ? logit : -INFINITY;
         float mx = x;
 #pragma unroll
         for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -416,8 +438,8 @@ __device__ __forceinline__ void generic_item(const PlanDevice& pd, const DeviceI
       }
     }
     __syncthreads();                              // the chunk's buffers (and, after the last one, the queries) are free
-    cur = nxt;
-    nxt = after;
+    cur = nxt; cur_pos = nxt_pos;
+    nxt = after; nxt_pos = after_pos;
   }
 #pragma unroll
   for (int i = 0; i < RPW; ++i) {
@@ -468,10 +490,10 @@ __device__ __forceinline__ void generic_append(const PlanDevice& pd, const T* __
 
 // (RPW for the plan's largest row block: an instance that chose per item was 65 to 79 KB of code, and a short launch
 // waits for its instructions.)
-template <typename T, int D, int RPW>
+template <typename T, int D, int RPW, bool SC>
 __global__ void __launch_bounds__(kGenThreads, 2) attn_generic_kernel(PlanDevice pd, const T* __restrict__ q, const T* __restrict__ k_new,
                                                                       const T* __restrict__ v_new, T* k_pool, T* v_pool, int n_q_heads,
-                                                                      int n_kv_heads, int page_size, float scale_log2) {
+                                                                      int n_kv_heads, int page_size, float scale_log2, float cap) {
   extern __shared__ __align__(1024) uint8_t gen_smem[];
   GenSmem<T, D>& sm = *reinterpret_cast<GenSmem<T, D>*>(gen_smem);
   pdl_launch_dependents();
@@ -486,7 +508,7 @@ __global__ void __launch_bounds__(kGenThreads, 2) attn_generic_kernel(PlanDevice
   }
   for (int idx = item_begin; idx < item_end; ++idx) {
     if (idx > item_begin) it = uniform_item(pd.items[idx]);
-    generic_item<T, D, RPW>(pd, it, sm, q, k_pool, v_pool, n_q_heads, n_kv_heads, page_size, scale_log2);
+    generic_item<T, D, RPW, SC>(pd, it, sm, q, k_pool, v_pool, n_q_heads, n_kv_heads, page_size, scale_log2, cap);
   }
 }
 
@@ -547,20 +569,26 @@ int launch_append(const aspd_plan* p, const void* k_new, const void* v_new, cons
                               sh.n_kv_heads, sh.head_dim, sh.page_size, p->dev));
 }
 
-template <typename T, int D, int RPW>
-static int launch_generic_rows(const aspd_plan* p, const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool,
+template <typename T, int D, int RPW, bool SC>
+static int launch_generic_instance(const aspd_plan* p, const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool,
                                cudaStream_t s) {
   static bool configured[64] = {};                 // the attribute belongs to the (function, device) pair
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return ASPD_ERR_CUDA;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    if (cudaFuncSetAttribute(attn_generic_kernel<T, D, RPW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GenSmem<T, D>)) != cudaSuccess)
+    if (cudaFuncSetAttribute(attn_generic_kernel<T, D, RPW, SC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GenSmem<T, D>)) != cudaSuccess)
       return ASPD_ERR_CUDA;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   const aspd_shape_t& sh = p->shape;
-  return status_of(launch_pdl(attn_generic_kernel<T, D, RPW>, dim3(p->n_ctas), dim3(kGenThreads), sizeof(GenSmem<T, D>), s, p->dev,
-                              (const T*)q, (const T*)k_new, (const T*)v_new, (T*)k_pool, (T*)v_pool, sh.n_q_heads, sh.n_kv_heads, sh.page_size, sh.sm_scale * kLog2e));
+  return status_of(launch_pdl(attn_generic_kernel<T, D, RPW, SC>, dim3(p->n_ctas), dim3(kGenThreads), sizeof(GenSmem<T, D>), s, p->dev,
+                              (const T*)q, (const T*)k_new, (const T*)v_new, (T*)k_pool, (T*)v_pool, sh.n_q_heads, sh.n_kv_heads, sh.page_size, SC ? sh.sm_scale : sh.sm_scale * kLog2e, p->cap));
+}
+template <typename T, int D, int RPW>
+static int launch_generic_rows(const aspd_plan* p, const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool,
+                               cudaStream_t s) {
+  return p->scored() ? launch_generic_instance<T, D, RPW, true>(p, q, k_new, v_new, k_pool, v_pool, s)
+                     : launch_generic_instance<T, D, RPW, false>(p, q, k_new, v_new, k_pool, v_pool, s);
 }
 template <typename T, int D>
 static int launch_generic(const aspd_plan* p, const void* q, const void* k_new, const void* v_new, const void* k_pool, const void* v_pool, cudaStream_t s) {

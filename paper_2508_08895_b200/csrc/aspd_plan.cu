@@ -372,16 +372,26 @@ int aspd_visible_slots_masked(const aspd_request_t* req, const aspd_branch_t* br
 
 static int plan_to_device(aspd_plan* p, cudaStream_t s);
 
+// Limits under which no logit overflows in fp32: a cap in log2 units, a slope times the largest distance.
+constexpr float kMostCap = 1e30f, kMostSlope = 1e30f;
+constexpr long kMostBiasPos = 1 << 24;      // position IDs are below that, so that their differences are exact in fp32
+
 // like: the plan that this one is to take the place of (aspd_plan_update re-plans on the host for the device that
 // plan lives on): the grid of its device, its way of splitting the streams and, as far as possible, of writing new rows
 // coarse: fewer and longer items, for host-only plans whose records would not fit into the static scratch otherwise
 static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req, const aspd_branch_t* br,
                             const int32_t* page_ids, int n_req, int64_t n_pool_pages, int mode, const int32_t* q_pos,
-                            const aspd_tuning_t* tuning, void* stream, const aspd_plan* like, bool coarse, aspd_plan_t** plan_out) {
+                            const aspd_tuning_t* tuning, const aspd_scores_t* scores, void* stream, const aspd_plan* like, bool coarse,
+                            aspd_plan_t** plan_out) {
   if (!plan_out) return ASPD_ERR_INVALID_ARG;
   *plan_out = nullptr;
   int rc = check_shape(shape);
   if (rc) return rc;
+  const float cap = scores ? scores->cap : 0.f;
+  const bool biased = scores && scores->slopes, rotated = scores && scores->rotated;
+  if (!(cap >= 0.f) || cap > kMostCap || (cap > 0.f && !(shape->sm_scale / cap <= 1e30f)) || (rotated && q_pos)) return ASPD_ERR_INVALID_ARG;
+  for (int h = 0; biased && h < shape->n_q_heads; ++h)
+    if (!(fabsf(scores->slopes[h]) <= kMostSlope)) return ASPD_ERR_INVALID_ARG;
   rc = check_counts(req, br, n_req, mode);
   if (rc) return rc;
   rc = check_layout(shape, req, br, page_ids, n_req, n_pool_pages, mode);
@@ -397,6 +407,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   if (tune.mask != ASPD_MASK_BRANCH_INVISIBLE && tune.mask != ASPD_MASK_SHARED) return ASPD_ERR_INVALID_ARG;
   if (tune.wide_rows != 0 && tune.wide_rows != 128 && tune.wide_rows != 256) return ASPD_ERR_INVALID_ARG;
   if (tune.mma_m != 0 && tune.mma_m != 64 && tune.mma_m != 96 && tune.mma_m != 128) return ASPD_ERR_INVALID_ARG;
+  if (tune.mma_m == 64 && (cap > 0.f || biased)) return ASPD_ERR_UNSUPPORTED;
   if (tune.combine != ASPD_COMBINE_AUTO && tune.combine != ASPD_COMBINE_KERNEL && tune.combine != ASPD_COMBINE_FUSED) return ASPD_ERR_INVALID_ARG;
   const bool shared_mask = tune.mask == ASPD_MASK_SHARED && mode == ASPD_MODE_BRANCH;
   const bool mma_ok = shape->dtype == ASPD_DTYPE_BF16;
@@ -415,6 +426,8 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   p->host_only = tune.host_only; p->n_pool_pages = n_pool_pages; p->device_base = nullptr; p->device_bytes = 0;
   memset(&p->dev, 0, sizeof(p->dev));
   p->tune = tune;
+  p->cap = cap; p->rotated = rotated ? 1 : 0;
+  if (biased) p->slopes.assign(scores->slopes, scores->slopes + Hq);
   p->sm_count = like ? like->sm_count : 148;
   if (!tune.host_only && !like) {
     int dev = 0, sms = 0;
@@ -429,6 +442,8 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   std::vector<int32_t> pos(n_new), slot(n_new), treq(n_new), tok_page(n_new), tok_row(n_new);
   rc = aspd_positions(req, br, n_req, mode, pos.data(), slot.data(), treq.data());
   if (rc) { delete p; return rc; }
+  if (biased) p->bias_pos = pos;
+  if (rotated) std::fill(pos.begin(), pos.end(), 0);
   for (int t = 0; t < n_new; ++t) {
     tok_page[t] = page_ids[req[treq[t]].page_begin + slot[t] / ps];
     tok_row[t] = slot[t] % ps;
@@ -447,13 +462,32 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   const int max_tok = std::max(1, kMaxRowsPerItem / G);
   struct Block { int request, tok0, n_tok, visit0, n_pages; };
   std::vector<int2> visit;
+  std::vector<int32_t> page_pos;                      // plans with a distance bias: position ID of every entry's first row
   std::vector<Block> blocks;
+  // Position ID of the first token of a region that is not the prefix (plans with a distance bias).
+  auto region_start = [&](const aspd_request_t& q, const aspd_branch_t& x) -> long {
+    if (x.pos_start != ASPD_POS_AUTO) return x.pos_start;
+    long s = q.prefix_len;
+    for (int b = 0; b < q.n_branches; ++b)
+      if (br[q.branch_begin + b].q_len == ASPD_Q_SHARED) s += br[q.branch_begin + b].kv_len;
+    return s;
+  };
+  for (int r = 0; biased && r < n_req; ++r) {
+    long total = req[r].prefix_len;
+    for (int b = 0; b < req[r].n_branches; ++b) {
+      const aspd_branch_t& x = br[req[r].branch_begin + b];
+      if (x.kv_len > 0 && x.q_len == ASPD_Q_SHARED && x.pos_start == ASPD_POS_AUTO) { delete p; return ASPD_ERR_BAD_DESCRIPTOR; }
+      if (region_start(req[r], x) + x.kv_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
+      total += x.kv_len;
+    }
+    if (total + req[r].tail_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
+  }
   std::vector<int4> tok_vis(n_new);
   int64_t kv_tokens = 0;
   const bool tok_field_fits = n_new < (1 << 18);      // the 18 bits above bit 13 of a page entry hold a token index
   bool counts_fit = true;                             // the 5 bits before them every page's number of new rows
   auto build_visit = [&](int block_tok) {
-    visit.clear(); blocks.clear();
+    visit.clear(); blocks.clear(); page_pos.clear();
     counts_fit = true;
     int64_t kv_count = 0;
     int t = 0;
@@ -463,7 +497,8 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
     // Under the shared mask the upper bits carry the page's index inside its branch instead (its
     // first key's offset / page_size; such plans never fuse the append): a token at offset k
     // also sees the keys of other branches whose offset is below k.
-    auto push_region = [&](const aspd_request_t& q, int slot0, int len, int new_key0, int new_tok0, bool branch_pages = false) {
+    // pos0: position ID of the region's first token (plans with a distance bias)
+    auto push_region = [&](const aspd_request_t& q, int slot0, int len, int new_key0, int new_tok0, long pos0, bool branch_pages = false) {
       const size_t at = visit.size();
       const int32_t* ids = page_ids + q.page_begin + slot0 / ps;
       const int n_old = (shared_mask && branch_pages) ? 0 : std::min(len, new_key0) / ps;       // full pages without new rows
@@ -481,12 +516,24 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
         else if (n_newrows > 0 && tok_field_fits) y |= (new_tok0 + first_new - new_key0) << 13;
         out[s0 / ps] = make_int2(ids[s0 / ps], y);
       }
+      if (biased)
+        for (size_t i = at; i < visit.size(); ++i) page_pos.push_back((int32_t)(pos0 + (long)(i - at) * ps));
+    };
+    // With a distance bias the prefix is walked from its end: a row's logits then fall along the stream and its first
+    // tile sets the reference maximum; the other way they rise by slope * 128 a tile and move it every tile.
+    auto push_prefix = [&](const aspd_request_t& q) {
+      const size_t at = visit.size();
+      push_region(q, 0, q.prefix_len, q.prefix_len, 0, 0);
+      if (biased) {
+        std::reverse(visit.begin() + at, visit.end());
+        std::reverse(page_pos.begin() + at, page_pos.end());
+      }
     };
     auto push_shared = [&](const aspd_request_t& q) {            // prefix and regions of earlier stages: seen by every branch
-      push_region(q, 0, q.prefix_len, q.prefix_len, 0);
+      push_prefix(q);
       for (int b = 0; b < q.n_branches; ++b) {
         const aspd_branch_t& x = br[q.branch_begin + b];
-        if (x.q_len == ASPD_Q_SHARED) push_region(q, x.kv_off, x.kv_len, x.kv_len, 0);
+        if (x.q_len == ASPD_Q_SHARED) push_region(q, x.kv_off, x.kv_len, x.kv_len, 0, region_start(q, x));
       }
     };
     for (int r = 0; r < n_req; ++r) {
@@ -509,7 +556,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
             const aspd_branch_t& x = br[q.branch_begin + b];
             if (x.q_len < 0 || (x.q_len == 0 && !shared_mask)) continue;     // shared mask: also branches without queries
             const int lo = ((int)visit.size() - v0) * ps, prior = x.kv_len - x.q_len;
-            push_region(q, x.kv_off, x.kv_len, prior, t, true);
+            push_region(q, x.kv_off, x.kv_len, prior, t, region_start(q, x), true);
             for (int i = 0; i < x.q_len; ++i) tok_vis[t++] = make_int4(pe, lo, lo + prior + i + 1, shared_mask ? prior + i : 0);
           }
           blocks.push_back({r, t_req, nq, v0, (int)visit.size() - v0});
@@ -523,6 +570,10 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
             } else {                                           // as in the request's first block
               visit.resize((size_t)bv0 + n_shared);
               std::copy(visit.begin() + v0, visit.begin() + v0 + n_shared, visit.begin() + bv0);
+              if (biased) {
+                page_pos.resize(visit.size());
+                std::copy(page_pos.begin() + v0, page_pos.begin() + v0 + n_shared, page_pos.begin() + bv0);
+              }
             }
             const int pe = n_shared * ps;
             int off = 0;                                       // index, among the request's new tokens, of the branch's first
@@ -532,7 +583,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
               const int a = std::max(blk0, off), e = std::min(blk1, off + x.q_len);
               if (a < e) {
                 const int lo = ((int)visit.size() - bv0) * ps, prior = x.kv_len - x.q_len;
-                push_region(q, x.kv_off, prior + (e - off), prior, t_req + off);   // up to the run's last token of this branch
+                push_region(q, x.kv_off, prior + (e - off), prior, t_req + off, region_start(q, x));   // up to the run's last token of this branch
                 for (int i = a - off; i < e - off; ++i) tok_vis[t_req + off + i] = make_int4(pe, lo, lo + prior + i + 1, 0);
               }
               off += x.q_len;
@@ -542,14 +593,15 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
           t += nq;
         }
       } else {
-        push_region(q, 0, q.prefix_len, q.prefix_len, 0);
+        push_prefix(q);
         kv_count += q.prefix_len + q.tail_len;
+        long written = q.prefix_len;
         for (int b = 0; b < q.n_branches; ++b) {
           const aspd_branch_t& x = br[q.branch_begin + b];
-          push_region(q, x.kv_off, x.kv_len, x.kv_len, 0);
-          kv_count += x.kv_len;
+          push_region(q, x.kv_off, x.kv_len, x.kv_len, 0, region_start(q, x));
+          kv_count += x.kv_len; written += x.kv_len;
         }
-        push_region(q, q.tail_off, q.tail_len, q.tail_len - 1, t);
+        push_region(q, q.tail_off, q.tail_len, q.tail_len - 1, t, written);
         tok_vis[t++] = make_int4(kCausalAll, 0, 0, 0);
         blocks.push_back({r, t_req, 1, v0, (int)visit.size() - v0});
       }
@@ -973,6 +1025,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   p->n_row_blocks = (int)row_blocks.size();
   p->visit.swap(visit); p->cta_item0.swap(cta_item0); p->part_base.swap(part_base); p->row_blocks.swap(row_blocks); p->q_pos.swap(pos);
   p->tok_vis.swap(tok_vis); p->tok_page.swap(tok_page); p->tok_row.swap(tok_row); p->dirty.swap(dirty); p->cta_dirty0.swap(cta_dirty0);
+  p->page_pos.swap(page_pos);
   if (tune.host_only) { *plan_out = p; return ASPD_OK; }
   rc = plan_to_device(p, (cudaStream_t)stream);
   if (rc) { delete p; return rc; }
@@ -983,13 +1036,19 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
 int aspd_plan_create(const aspd_shape_t* shape, const aspd_request_t* req, const aspd_branch_t* br,
                      const int32_t* page_ids, int n_req, int64_t n_pool_pages, int mode, const int32_t* q_pos,
                      const aspd_tuning_t* tuning, void* stream, aspd_plan_t** plan_out) {
-  const int rc = plan_create_impl(shape, req, br, page_ids, n_req, n_pool_pages, mode, q_pos, tuning, stream, nullptr, false, plan_out);
+  return aspd_plan_create_scores(shape, req, br, page_ids, n_req, n_pool_pages, mode, q_pos, tuning, nullptr, stream, plan_out);
+}
+
+int aspd_plan_create_scores(const aspd_shape_t* shape, const aspd_request_t* req, const aspd_branch_t* br,
+                            const int32_t* page_ids, int n_req, int64_t n_pool_pages, int mode, const int32_t* q_pos,
+                            const aspd_tuning_t* tuning, const aspd_scores_t* scores, void* stream, aspd_plan_t** plan_out) {
+  const int rc = plan_create_impl(shape, req, br, page_ids, n_req, n_pool_pages, mode, q_pos, tuning, scores, stream, nullptr, false, plan_out);
   if (rc || !tuning || !tuning->host_only || fits_static_scratch(*plan_out)) return rc;
   // Cut for speed, the CUDA-core kernel's steps have up to two items per SM and so twice the records of steps that
   // give every SM one share: 28/4 heads of 128 in fp32, 16 tokens over 3 k, 9.9 MB instead of 5.0.  A host-only plan
   // that aspd_attn_static could not take is made again with those.
   aspd_plan_t* longer = nullptr;
-  if (plan_create_impl(shape, req, br, page_ids, n_req, n_pool_pages, mode, q_pos, tuning, stream, nullptr, true, &longer) != ASPD_OK) return rc;
+  if (plan_create_impl(shape, req, br, page_ids, n_req, n_pool_pages, mode, q_pos, tuning, scores, stream, nullptr, true, &longer) != ASPD_OK) return rc;
   if (fits_static_scratch(longer)) std::swap(longer, *plan_out);
   delete longer;
   return rc;
@@ -1018,6 +1077,10 @@ static void plan_layout(const aspd_plan* p, double slack, aspd::PlanLayout* L) {
   L->o_rb = take(sizeof(int2) * std::max<size_t>(1, p->row_blocks.size()));
   L->o_pbase = take(sizeof(int32_t) * p->part_base.size());
   L->o_freq = take(sizeof(double) * (d / 2));
+  const bool biased = !p->slopes.empty();
+  L->o_ppos = take(biased ? sizeof(int32_t) * L->cap_visit : 0);
+  L->o_bpos = take(biased ? sizeof(int32_t) * std::max(1, n_new) : 0);
+  L->o_slope = take(sizeof(float) * p->slopes.size());
   L->upload_bytes = off;
   // the status word is zeroed when the plan is created and never uploaded again, so that a time-out
   // recorded by an earlier launch survives aspd_plan_update until aspd_plan_status reads it
@@ -1056,6 +1119,11 @@ static int plan_upload(aspd_plan* p, cudaStream_t s, bool clear) {
   memcpy(blob + L.o_pbase, p->part_base.data(), sizeof(int32_t) * p->part_base.size());
   double* freq = reinterpret_cast<double*>(blob + L.o_freq);
   for (int i = 0; i < d / 2; ++i) freq[i] = pow((double)p->shape.rope_theta, -2.0 * i / d);
+  if (!p->slopes.empty()) {
+    if (!p->page_pos.empty()) memcpy(blob + L.o_ppos, p->page_pos.data(), sizeof(int32_t) * p->page_pos.size());
+    if (n_new) memcpy(blob + L.o_bpos, p->bias_pos.data(), sizeof(int32_t) * n_new);
+    fill_slopes(p, reinterpret_cast<float*>(blob + L.o_slope));
+  }
   size_t bytes = L.upload_bytes;
   if (clear) {                                     // the status word and the counters lie right behind the tables: one copy
     memset(blob + L.o_status, 0, L.cleared_end - L.o_status);
@@ -1088,6 +1156,11 @@ static int plan_to_device(aspd_plan* p, cudaStream_t s) {
   p->dev.q_cs = (const float2*)(b8 + L.o_qcs);
   p->dev.part_base = (const int32_t*)(b8 + L.o_pbase);
   p->dev.inv_freq = (const double*)(b8 + L.o_freq);
+  if (!p->slopes.empty()) {
+    p->dev.page_pos = (const int32_t*)(b8 + L.o_ppos);
+    p->dev.bias_pos = (const int32_t*)(b8 + L.o_bpos);
+    p->dev.slopes = (const float*)(b8 + L.o_slope);
+  }
   p->dev.status = (int32_t*)(b8 + L.o_status);
   p->dev.work_counter = p->dev.status + 1;
   p->dev.arrive = (int32_t*)(b8 + L.o_arrive);
@@ -1107,7 +1180,8 @@ int aspd_plan_update(aspd_plan_t* p, const aspd_request_t* req, const aspd_branc
   aspd_tuning_t tune = p->tune;
   tune.host_only = 1;
   aspd_plan* t = nullptr;
-  int rc = plan_create_impl(&p->shape, req, br, page_ids, n_req, p->n_pool_pages, p->mode, q_pos, &tune, nullptr, p, false, &t);
+  const aspd_scores_t scores = {p->cap, p->slopes.empty() ? nullptr : p->slopes.data(), p->rotated};
+  int rc = plan_create_impl(&p->shape, req, br, page_ids, n_req, p->n_pool_pages, p->mode, q_pos, &tune, &scores, nullptr, p, false, &t);
   if (rc) return rc;
   const aspd::PlanLayout& L = p->layout;
   if (t->n_new != p->n_new || t->n_ctas != p->n_ctas || t->base_ctas != p->base_ctas || t->kernel != p->kernel || t->wide != p->wide || t->dealt != p->dealt ||
@@ -1128,6 +1202,7 @@ int aspd_plan_update(aspd_plan_t* p, const aspd_request_t* req, const aspd_branc
   p->items.swap(t->items); p->visit.swap(t->visit); p->tok_vis.swap(t->tok_vis); p->cta_item0.swap(t->cta_item0);
   p->part_base.swap(t->part_base); p->q_pos.swap(t->q_pos); p->row_blocks.swap(t->row_blocks);
   p->tok_page.swap(t->tok_page); p->tok_row.swap(t->tok_row); p->cta_dirty0.swap(t->cta_dirty0); p->dirty.swap(t->dirty);
+  p->page_pos.swap(t->page_pos); p->bias_pos.swap(t->bias_pos);
   delete t;
   return plan_upload(p, (cudaStream_t)stream, false);
 }

@@ -46,7 +46,7 @@ constexpr size_t kStatusOffset = kScratchBytes - 256;
 
 // Where the tables and the split-K workspace lie inside the scratch array.
 struct StaticLayout {
-  size_t items, cta, visit, tvis, rb, qcs, pbase, upload_bytes, wso, wsml, end;
+  size_t items, cta, visit, tvis, rb, qcs, pbase, ppos, bpos, slope, upload_bytes, wso, wsml, end;
 };
 StaticLayout static_layout(const aspd_plan* p) {
   const int d = p->shape.head_dim, G = p->shape.n_q_heads / p->shape.n_kv_heads;
@@ -60,6 +60,9 @@ StaticLayout static_layout(const aspd_plan* p) {
   L.rb = take(sizeof(int2) * p->row_blocks.size());
   L.qcs = take(sizeof(float2) * (size_t)p->n_new * (d / 2));
   L.pbase = take(sizeof(int32_t) * p->part_base.size());
+  L.ppos = take(sizeof(int32_t) * p->page_pos.size());
+  L.bpos = take(sizeof(int32_t) * p->bias_pos.size());
+  L.slope = take(sizeof(float) * p->slopes.size());
   L.upload_bytes = off;
   L.wso = take(sizeof(float) * (size_t)p->n_partials * G * d);
   L.wsml = take(sizeof(float2) * (size_t)p->n_partials * G);
@@ -104,6 +107,11 @@ extern "C" int aspd_attn_static(const aspd_plan_t* plan, const void* q, const vo
   memcpy(blob.data() + L.tvis, plan->tok_vis.data(), sizeof(int4) * plan->tok_vis.size());
   memcpy(blob.data() + L.rb, plan->row_blocks.data(), sizeof(int2) * plan->row_blocks.size());
   memcpy(blob.data() + L.pbase, plan->part_base.data(), sizeof(int32_t) * plan->part_base.size());
+  if (!plan->slopes.empty()) {
+    memcpy(blob.data() + L.ppos, plan->page_pos.data(), sizeof(int32_t) * plan->page_pos.size());
+    memcpy(blob.data() + L.bpos, plan->bias_pos.data(), sizeof(int32_t) * plan->bias_pos.size());
+    aspd::fill_slopes(plan, reinterpret_cast<float*>(blob.data() + L.slope));
+  }
   float2* qcs = reinterpret_cast<float2*>(blob.data() + L.qcs);
   double inv_freq[64];
   for (int i = 0; i < d / 2; ++i) inv_freq[i] = pow((double)sh.rope_theta, -2.0 * i / d);
@@ -126,6 +134,7 @@ extern "C" int aspd_attn_static(const aspd_plan_t* plan, const void* q, const vo
   shell.sm_count = plan->sm_count; shell.n_row_blocks = plan->n_row_blocks; shell.stable_cache = 0; shell.fuse_append = 0; shell.n_pool_pages = plan->n_pool_pages;
   shell.kv_tokens_read = plan->kv_tokens_read; shell.algorithmic_bytes = plan->algorithmic_bytes;
   shell.dealt = plan->dealt; shell.wide = plan->wide; shell.shared_mask = plan->shared_mask; shell.m64 = plan->m64; shell.dec = plan->dec; shell.max_rows = plan->max_rows; shell.max_parts = plan->max_parts;   // which kernel variant the items were made for
+  shell.cap = plan->cap; shell.slopes = plan->slopes;
   shell.device_bytes = 0; shell.device_base = nullptr;
   memset(&shell.dev, 0, sizeof(shell.dev));
   shell.dev.items = (const DeviceItem*)(base + L.items);
@@ -135,6 +144,11 @@ extern "C" int aspd_attn_static(const aspd_plan_t* plan, const void* q, const vo
   shell.dev.row_blocks = (const int2*)(base + L.rb);
   shell.dev.q_cs = (const float2*)(base + L.qcs);
   shell.dev.part_base = (const int32_t*)(base + L.pbase);
+  if (!plan->slopes.empty()) {
+    shell.dev.page_pos = (const int32_t*)(base + L.ppos);
+    shell.dev.bias_pos = (const int32_t*)(base + L.bpos);
+    shell.dev.slopes = (const float*)(base + L.slope);
+  }
   shell.dev.status = (int32_t*)(base + kStatusOffset);
   shell.dev.work_counter = shell.dev.status + 1;
   shell.dev.ws_o = (float*)(base + L.wso);
