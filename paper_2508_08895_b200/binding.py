@@ -258,7 +258,7 @@ class Plan:
                  chunk_tokens: int = 0, n_ctas: int = 0, host_only: bool = False, stable_cache: bool = False, stream=None,
                  mask: int = 0, updatable: bool = False, combine: int = COMBINE_AUTO, wide_rows: int = 0, mma_m: int = 0,
                  scores: Optional[Scores] = None):
-        self.shape, self.mode = shape, mode
+        self.shape, self.mode, self._dims = shape, mode, None
         req, br, pages = pack_descriptors(desc)
         tune = Tuning(kernel, chunk_tokens, n_ctas, 1 if host_only else 0, 1 if stable_cache else 0, mask, 1 if updatable else 0, combine, wide_rows, mma_m)
         qp = None if q_pos is None else np.ascontiguousarray(q_pos, dtype=np.int32)
@@ -272,6 +272,16 @@ class Plan:
         self.info = PlanInfo()
         _check(lib().aspd_plan_info(self._h, ctypes.addressof(self.info)), "aspd_plan_info")
         self.n_new = self.info.n_new
+
+    def _rows(self):
+        """Shapes of q and of k_new / v_new, elements of q, torch's storage type and int32: made once (a field of a ctypes
+        struct takes as long as a tensor's check)."""
+        if self._dims is None:
+            import torch
+            sh = self.shape
+            shapes = [torch.Size((self.n_new, h, sh.head_dim)) for h in (sh.n_q_heads, sh.n_kv_heads)]
+            self._dims = *shapes, shapes[0].numel(), torch.bfloat16 if sh.dtype == DTYPE_BF16 else torch.float32, torch.int32
+        return self._dims
 
     def update(self, desc, q_pos=None, stream=None) -> None:
         """Re-plan in place for the next step of the same batch (see ``aspd_plan_update``)."""
@@ -356,32 +366,33 @@ class QkNorm:
         self.weights = q_weight, k_weight           # kept alive
         self.n_axes = max(axes) + 1
         self.c = _QkNorm(_ptr(q_weight), _ptr(k_weight), eps, self.n_axes, 1 if rotate_q else 0, (ctypes.c_uint8 * 64)(*axes))
+        self.address = ctypes.addressof(self.c)
 
 
 def _esize(shape: Shape) -> int:
     return 2 if shape.dtype == DTYPE_BF16 else 4
 
 
-def _token_stride(x, shape: Shape, heads: int, n: int) -> int:
+def _token_stride(x, dtype, shape) -> int:
     """Elements from one token's heads to the next one's; the heads of a token must lie together."""
-    row = heads * shape.head_dim
-    inner = x.stride()[1:] == (shape.head_dim, 1) if x.dim() == 3 else x.dim() == 2 and x.stride(1) == 1
-    if x.shape[0] != n or x.numel() != n * row or not (inner or (x.dim() == 3 and heads == 1 and x.stride(2) == 1)) or x.element_size() != _esize(shape):
+    stride = x.stride()
+    if x.dtype is not dtype or stride[-1] != 1 or not (x.shape == shape and (stride[1] == shape[2] or shape[1] == 1) or
+                                                       x.shape == (shape[0], shape[1] * shape[2])):
         raise ValueError("tokens: [n_new][heads][head_dim] of the storage type, the heads of a token together")
-    return x.stride(0) if n > 1 else row
+    return stride[0]
 
 
 def qk_norm_append(plan: Plan, norm: QkNorm, q, k_new, v_new, pos, k_pool, v_pool, q_out, stream=None) -> None:
     """Norms, rotation and paged append of the step's new tokens (see ``aspd_qk_norm_append``).  q, k_new, v_new may be
     views of one packed projection; pos: device int32 [n_axes][n_new]."""
-    sh, n = plan.shape, plan.n_new
-    if pos.numel() < norm.n_axes * n or not pos.is_contiguous() or pos.element_size() != 4:
+    q_shape, kv_shape, q_size, dtype, int32 = plan._rows()
+    if pos.numel() < norm.n_axes * q_shape[0] or pos.dtype is not int32 or not pos.is_contiguous():
         raise ValueError("pos: contiguous int32 [n_axes][n_new]")
-    strides = [_token_stride(x, sh, h, n) for x, h in ((q, sh.n_q_heads), (k_new, sh.n_kv_heads), (v_new, sh.n_kv_heads))]
-    if q_out.numel() != n * sh.n_q_heads * sh.head_dim or not q_out.is_contiguous() or q_out.element_size() != _esize(sh):
+    qs, ks, vs = _token_stride(q, dtype, q_shape), _token_stride(k_new, dtype, kv_shape), _token_stride(v_new, dtype, kv_shape)
+    if q_out.numel() != q_size or q_out.dtype is not dtype or not q_out.is_contiguous():
         raise ValueError("q_out: contiguous [n_new][n_q_heads][head_dim] of the storage type")
-    _check(lib().aspd_qk_norm_append(plan._h, ctypes.addressof(norm.c), _ptr(q), strides[0], _ptr(k_new), strides[1], _ptr(v_new), strides[2],
-                                     _ptr(pos), _ptr(k_pool), _ptr(v_pool), _ptr(q_out), _stream(stream)), "aspd_qk_norm_append")
+    _check(lib().aspd_qk_norm_append(plan._h, norm.address, q.data_ptr(), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, pos.data_ptr(),
+                                     k_pool.data_ptr(), v_pool.data_ptr(), q_out.data_ptr(), _stream(stream)), "aspd_qk_norm_append")
 
 
 def branch_attn(plan: Plan, q, k_pool, v_pool, out, stream=None) -> None:
