@@ -124,7 +124,7 @@ typedef struct {
   int32_t wide_rows;    /* plans that deal whole streams to the tensor-core kernel: query rows of a row
                            block, 128 (one tile) or 256 (two tiles scored against every K/V tile the CTA
                            fetches); 0 = automatic (256 when a request has more query tokens than one
-                           tile holds)                                                                */
+                           tile holds).  Always 128 for scores capped above 55 or capped with a rising bias   */
   int32_t mma_m;        /* stream-K plans of the tensor-core kernel: M of its MMAs, 128 (the at most 64 query
                            rows of a row block are replicated to fill 128 accumulator rows), 64 (half the
                            tensor work; the accumulators then use 16 lanes of each quadrant) or 96, which
@@ -270,7 +270,7 @@ typedef struct {
 } aspd_scores_t;
 /*
  * aspd_plan_create with these options (scores = NULL: the same).  ASPD_ERR_INVALID_ARG for a cap that is
- * negative, above 1e30, or below sm_scale / 1e30; for slopes above 1e30 in magnitude or not finite; for q_pos with
+ * negative, above 1e30, or below sm_scale / 1e30; for slopes above 32 in magnitude or not finite; for q_pos with
  * rotated.  ASPD_ERR_UNSUPPORTED for a cap or slopes with tuning->mma_m = 64.  With slopes, ASPD_ERR_TOO_LARGE for
  * position IDs of 2^24 and more.
  */

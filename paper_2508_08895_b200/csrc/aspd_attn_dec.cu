@@ -293,8 +293,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
     if constexpr (SC) {
       const ScoreMisc* sm = reinterpret_cast<const ScoreMisc*>(misc + 1);
       if (c.sp.cap_in != 0.f) {
-#pragma unroll
-        for (int i = 0; i < HC; ++i) s[i] = capped(s[i], c.sp);
+        cap_scores(s, c.sp);
       } else {
 #pragma unroll
         for (int i = 0; i < HC; ++i) s[i] *= c.sp.scale;

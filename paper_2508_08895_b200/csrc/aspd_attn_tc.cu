@@ -1324,9 +1324,12 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
     auto all = [&](auto sc) {
       constexpr bool SC = decltype(sc)::value;
       return attr(attn_tc_kernel<false, kPlain, SC>, kSmemBytes) && attr(attn_tc_kernel<false, kOptions, SC>, kSmemBytes) &&
-             attr(attn_tc_kernel<false, kPatch, SC>, kSmemBytes) && attr(attn_tc_kernel<true, kPlain, SC>, kSmemBytes) && attr(attn_tc_w2_kernel<SC>, kSmemBytesW2);
+             attr(attn_tc_kernel<false, kPatch, SC>, kSmemBytes) && attr(attn_tc_kernel<true, kPlain, SC>, kSmemBytes);
     };
-    if (!all(std::false_type()) || !all(std::true_type())) return ASPD_ERR_CUDA;
+    if (!all(std::false_type()) || !all(std::true_type()) || !attr(attn_tc_w2_kernel<kPlainScores>, kSmemBytesW2) ||
+        !attr(attn_tc_w2_kernel<kCapped>, kSmemBytesW2) || !attr(attn_tc_w2_kernel<kBiased>, kSmemBytesW2) ||
+        !attr(attn_tc_w2_kernel<kCapped | kBiased>, kSmemBytesW2))
+      return ASPD_ERR_CUDA;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   Ctx c;
@@ -1358,8 +1361,11 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
   if (p->wide == 2) {                       // row blocks of two query tiles: final outputs only
     if (c.out == nullptr) return ASPD_ERR_UNSUPPORTED;
     c.k_new = nullptr; c.v_new = nullptr;
-    return launch_pdl(p->scored() ? attn_tc_w2_kernel<true> : attn_tc_w2_kernel<false>, dim3(p->n_ctas), dim3(kThreadsW2), kSmemBytesW2, s, c) == cudaSuccess
-               ? ASPD_OK : ASPD_ERR_CUDA;
+    const bool biased = !p->slopes.empty();
+    if (p->cap == 0.f) c.scale_log2 = c.sp.scale;      // (this kernel's instances without a cap scale as the plain one does)
+    auto* w2 = p->cap > 0.f ? (biased ? attn_tc_w2_kernel<kCapped | kBiased> : attn_tc_w2_kernel<kCapped>)
+                            : (biased ? attn_tc_w2_kernel<kBiased> : attn_tc_w2_kernel<kPlainScores>);
+    return launch_pdl(w2, dim3(p->n_ctas), dim3(kThreadsW2), kSmemBytesW2, s, c) == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
   }
   auto instance = [&](auto sc) {
     constexpr bool SC = decltype(sc)::value;

@@ -110,8 +110,72 @@ __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok
   fence_async_smem();
 }
 
+// What a plan's scores are, beside the plain products (see aspd_scores.cuh); an instance of the kernel for each.
+enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
+
+// A half whose scores reach beyond the short polynomial, 16 at a time out of tensor memory and their P back over scores that have
+// been read (P of scores 16 i ... takes columns 8 i ...): the longer polynomial up to the cap, two more special functions a score
+// beyond.  Returned: the row's sum.  A loop, and a short one, on purpose: the passes are straight code, and forms of
+// them taken in turn did not fit the instruction cache (products up to the cap and beyond it in one step, 25 % more passes:
+// 1 280 -> 3 885 us).
+template <bool BIAS>
+__device__ __forceinline__ float far_half(const Ctx& c, const MiscW2* misc, const RowBias& rb, const int4& vis, uint32_t s_addr, int ring, int page0, int kb0,
+                                          float& top) {
+  float2 sum = make_float2(0.f, 0.f);
+  top = 0.f;
+#pragma unroll 1
+  for (int q = 0; q < 4; ++q) {
+    float s[16];
+    ASPD_TMEM_LD16(s_addr + q * 16, s, 0);
+    const int nv = misc->nval[ring][page0 + q] & 255, kb = kb0 + q * 16;
+    const uint32_t mask = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb));
+    float2 dist = make_float2(0.f, 0.f);
+    if constexpr (BIAS) {
+      dist.x = (float)(misc->kpos[ring][page0 + q] - rb.pos);
+      dist.y = dist.x + 1.f;
+    }
+    tmem_wait_ld16(s);
+    float mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mx = fmaxf(mx, fmaxf(fabsf(s[i]), fabsf(s[i + 1])));
+    top = fmaxf(top, mx);
+    if (__any_sync(0xffffffffu, mx > c.sp.poly_limit)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = saturated(s[i], c.sp);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float2 z = __fmul2_rn(make_float2(s[i], s[i + 1]), make_float2(c.sp.cap_in, c.sp.cap_in)), u = __fmul2_rn(z, z);
+        float2 p = make_float2(c.sp.poly[5], c.sp.poly[5]);
+#pragma unroll
+        for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.poly[k], c.sp.poly[k]));
+        p = __fmul2_rn(p, z);
+        s[i] = p.x; s[i + 1] = p.y;
+      }
+    }
+    uint32_t p8[8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      float2 x = make_float2(s[i], s[i + 1]);
+      if constexpr (BIAS) {
+        x = __ffma2_rn(make_float2(rb.slope, rb.slope), dist, x);
+        dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
+      }
+      x.x = ex2((mask >> i) & 1u ? x.x : -INFINITY);
+      x.y = ex2((mask >> (i + 1)) & 1u ? x.y : -INFINITY);
+      sum = __fadd2_rn(sum, x);
+      p8[i >> 1] = pack_bf16(x.x, x.y);
+    }
+    ASPD_TMEM_ST8U(s_addr + q * 8, p8);
+  }
+  return sum.x + sum.y;
+}
+
 // One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.
-template <bool SC>
+// SC: kCapped | kBiased.  Capped scores come here only with fixed references (fixed_reference): the exponentials are taken against 0
+// always.  A half is one pass with the short polynomial, which keeps the largest product; where that turns out to be beyond the
+// polynomial's range (scores above 0.6 of the cap) the half is taken again by far_half, and the warp's next half goes there at once.
+template <int SC>
 __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                  int item_end, int grp, int tpt) {
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, r = tid & 127;
@@ -145,9 +209,10 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
     const int tl = token_of(c, r), M = n_tok * G, tok = it.q_tok0 + grp * tpt + tl;
     int4 vis = make_int4(0, 0, 0, 0);                          // padding rows see nothing
     if (r < M) vis = c.pd.tok_vis[tok];
+    constexpr bool CAP = SC & kCapped, BIAS = SC & kBiased;
     RowBias rb = {0.f, 0};
-    const bool biased = SC && c.pd.slopes != nullptr;
-    if (biased && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
+    if (BIAS && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
+    bool far = false;                                           // the warp's last half had scores beyond the short polynomial
     float m_ref = 0.f, l = 0.f;                                 // see the one-tile variant: the reference starts at 0
     bool seen = r >= M;                                         // padding rows never need the tracking pass
     bool warp_seen = false;                                     // all rows of the warp have (kept up in the full path only)
@@ -182,11 +247,30 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
         // then (and for rows that have not seen a key yet) finds the maximum.
         const int kb0 = kbt + h * 64;
         const bool masked = h ? masked1 : masked0;
-        auto pass_impl = [&](float ref, auto track_tag, auto masked_tag) {
-          constexpr bool TRACK = decltype(track_tag)::value, MASKED = decltype(masked_tag)::value;
+        float top;                                  // capped: largest product
+        // KIND: exponents against a reference and their largest (kTracked) or not (kPlainPass); kNear: capped
+        enum { kPlainPass, kTracked, kNear };
+        auto pass_impl = [&](float ref, auto kind_tag, auto masked_tag) {
+          constexpr int KIND = decltype(kind_tag)::value;
+          constexpr bool TRACK = KIND == kTracked, MASKED = decltype(masked_tag)::value;
+          if (CAP) top = 0.f;
           float mx0 = -INFINITY, mx1 = -INFINITY;
           float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0, sum2 = sum0, sum3 = sum0;
-          const float2 sc2 = make_float2(c.scale_log2, c.scale_log2), nb2 = make_float2(-ref, -ref);
+          const float2 sc2 = make_float2(c.scale_log2, c.scale_log2), nb2 = make_float2(-ref, -ref), sl2 = make_float2(rb.slope, rb.slope);
+          // logits less the reference
+          auto exponents = [&](float a, float b, float2 less) {
+            const float2 x = make_float2(a, b);
+            if constexpr (KIND == kNear) {
+              top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+              const float2 u = __fmul2_rn(x, x);
+              float2 p = make_float2(c.sp.near[3], c.sp.near[3]);
+#pragma unroll
+              for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.near[k], c.sp.near[k]));
+              return __ffma2_rn(x, p, less);
+            } else {
+              return __ffma2_rn(x, sc2, less);
+            }
+          };
           float s0[32], s1[32];
           ASPD_TMEM_LD32(s_base + h * 64, s0, 0);
           tmem_wait_ld32(s0);
@@ -194,18 +278,33 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 #pragma unroll
           for (int ch = 0; ch < 2; ++ch) {
             if (ch == 1) tmem_wait_ld32(s1);
-            float (&s)[32] = ch ? s1 : s0;
-            if constexpr (SC) score_row(s, c.sp, biased, rb, &misc->kpos[g & (kPageRingW2 - 1)][4 * h + 2 * ch]);
+            const float (&s)[32] = ch ? s1 : s0;
 #pragma unroll
             for (int pg = 0; pg < 2; ++pg) {
               const int nv = (h ? ye8[4 + ch * 2 + pg] : ye8[ch * 2 + pg]) & 255;
               const int kb = kb0 + ch * 32 + pg * 16;
               uint32_t mask = 0xFFFFu;
               if constexpr (MASKED) mask = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb));
+              // the bias less the reference, two keys at a time; distances in whole numbers (a steep slope times a rounded one
+              // would not be 0 at the row's own key)
+              float2 dist = make_float2(0.f, 0.f);
+              if constexpr (BIAS) {
+                dist.x = (float)(misc->kpos[g & (kPageRingW2 - 1)][4 * h + 2 * ch + pg] - rb.pos);
+                dist.y = dist.x + 1.f;
+              }
+              auto less = [&] {
+                if constexpr (BIAS) {
+                  const float2 b = __ffma2_rn(sl2, dist, nb2);
+                  dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
+                  return b;
+                } else {
+                  return nb2;
+                }
+              };
 #pragma unroll
               for (int i = 0; i < 16; i += 4) {
-                float2 x0 = __ffma2_rn(make_float2(s[pg * 16 + i], s[pg * 16 + i + 1]), sc2, nb2);
-                float2 x1 = __ffma2_rn(make_float2(s[pg * 16 + i + 2], s[pg * 16 + i + 3]), sc2, nb2);
+                float2 x0 = exponents(s[pg * 16 + i], s[pg * 16 + i + 1], less());
+                float2 x1 = exponents(s[pg * 16 + i + 2], s[pg * 16 + i + 3], less());
                 if (MASKED && mask != 0xFFFFu) {
                   x0.x = (mask >> i) & 1u ? x0.x : -INFINITY;
                   x0.y = (mask >> (i + 1)) & 1u ? x0.y : -INFINITY;
@@ -225,20 +324,34 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
           tile_sum = st.x + st.y;
           tmax = fmaxf(mx0, mx1);
         };
-        auto pass = [&](float ref, auto track_tag) {
-          if (masked) pass_impl(ref, track_tag, std::true_type());
-          else pass_impl(ref, track_tag, std::false_type());
+        if constexpr (CAP) {
+          bool again = far;
+          if (!again) {
+            if (masked) pass_impl(0.f, std::integral_constant<int, kNear>(), std::true_type());
+            else pass_impl(0.f, std::integral_constant<int, kNear>(), std::false_type());
+            again = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
+          }
+          if (again) {
+            tile_sum = far_half<BIAS>(c, misc, rb, vis, s_base + h * 64, g & (kPageRingW2 - 1), 4 * h, kb0, top);
+            far = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
+          } else {
+            ASPD_TMEM_ST32U(s_base + h * 64, pk, 0);
+          }
+        } else {
+        auto pass = [&](float ref, auto kind_tag) {
+          if (masked) pass_impl(ref, kind_tag, std::true_type());
+          else pass_impl(ref, kind_tag, std::false_type());
         };
         // The common case -- every row of the warp has seen a key and no exponent passed 2^40 -- is
         // the plain pass and one vote; everything else goes the full way.
         bool settled = false;
         if (warp_seen) {
-          pass(m_ref, std::false_type());
+          pass(m_ref, std::integral_constant<int, kPlainPass>());
           // an exponent beyond 2^40 makes the sum exceed it (the converse is harmless: one more pass)
           settled = !__any_sync(0xffffffffu, !(tile_sum <= kRaiseSumW2));
         }
         if (!settled) {
-          pass(m_ref, std::true_type());
+          pass(m_ref, std::integral_constant<int, kTracked>());
           // move the reference: up when an exponent passed 2^40; down only while the row has not seen a
           // key yet (l and its row of O are still exactly 0 then, so nothing is rescaled)
           const bool raise = tmax > kRaiseW2, lower = !seen && tmax < -kLower && tmax > -INFINITY;
@@ -264,14 +377,15 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
               }
               tmem_wait_st();
             }
-            pass(m_ref, std::false_type());           // the whole warp again (TMEM loads are warp-wide)
+            pass(m_ref, std::integral_constant<int, kPlainPass>());           // the whole warp again (TMEM loads are warp-wide)
           }
+        }
+        ASPD_TMEM_ST32U(s_base + h * 64, pk, 0);
         }
         l += tile_sum;
         if (tid == 0) ASPD_STAMP(c, g, 4 * h + 1);
-        // the half's P (64 bf16 = 32 columns) over its own scores, which nobody needs any more: the next
-        // scores go there behind the P.V that reads it, from the same issuer
-        ASPD_TMEM_ST32U(s_base + h * 64, pk, 0);
+        // (the half's P, 64 bf16 = 32 columns, lies over its own scores, which nobody needs any more: the next
+        // scores go there behind the P.V that reads it, from the same issuer)
         tmem_wait_st();
         tc_fence_before();
         warp_arrive_w2(bar_pfull + 8 * h);
@@ -322,7 +436,7 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 }
 
 
-template <bool SC>
+template <int SC>
 __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -338,7 +452,7 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   const int item_begin = uniform(head.x), item_end = uniform(head.y);
   int2 first_pages = make_int2(0, 0);
   if ((warp == W2_KPROD || warp == W2_VPROD) && lane < head.w) first_pages = c.pd.visit[head.z + lane];
-  const bool page_positions = SC && warp == W2_KPROD && c.pd.page_pos != nullptr;
+  const bool page_positions = (SC & kBiased) && warp == W2_KPROD;
   int first_pos = 0;
   if (page_positions && lane < head.w) first_pos = c.pd.page_pos[head.z + lane];
   {
@@ -390,7 +504,7 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
         if ((t & 3) == 0) {
           cur = nxt;
           nxt = make_int2(0, 0);
-          if constexpr (SC) { cur_pos = nxt_pos; nxt_pos = 0; }
+          if constexpr (SC & kBiased) { cur_pos = nxt_pos; nxt_pos = 0; }
           const int ahead = (t + 4) * 8 + lane;
           if ((t + 4) * 8 < it.n_pages) {
             if (ahead < it.n_pages) nxt = c.pd.visit[it.page0 + ahead];
@@ -418,7 +532,7 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
         if (!good) { ok = false; break; }
         if (lane == 0) ASPD_STAMP(c, g, 13 + kv);
         if (kv == 0 && lane < 8) misc->nval[g & (kPageRingW2 - 1)][lane] = pg.y;   // read by the softmax groups of tile g
-        if constexpr (SC) {
+        if constexpr (SC & kBiased) {
           const int kp = __shfl_sync(0xffffffffu, cur_pos, (t & 3) * 8 + (lane & 7));
           if (page_positions && lane < 8) misc->kpos[g & (kPageRingW2 - 1)][lane] = kp;
         }

@@ -235,6 +235,15 @@ inline void fill_cta_head(const aspd_plan* p, int4* dst) {
     dst[2 * c + 1] = make_int4(p->cta_dirty0[c], p->cta_dirty0[c + 1] - p->cta_dirty0[c], 0, 0);
   }
 }
+// Softmax weights of a capped row need no maximum: its logits lie within +-cap, a bias with slopes of 0 and more only lowers them, and
+// the row's own key, at distance 0, is not lowered at all.  Up to this cap in log2 units (scores up to 55) weights taken against 0
+// neither overflow in sums over 2^24 keys times values of 2^20, nor vanish where they matter.
+constexpr float kFixedCap = 80.f;
+inline bool fixed_reference(const aspd_plan* p) {
+  bool falling = true;
+  for (float s : p->slopes) falling = falling && s >= 0.f;
+  return p->cap > 0.f && p->cap * 1.4426950408889634f <= kFixedCap && falling;
+}
 // the device plan's slopes, from the host's
 inline void fill_slopes(const aspd_plan* p, float* dst) {
   for (size_t h = 0; h < p->slopes.size(); ++h) dst[h] = p->slopes[h] * 1.4426950408889634f;

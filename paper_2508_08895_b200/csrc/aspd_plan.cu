@@ -372,9 +372,10 @@ int aspd_visible_slots_masked(const aspd_request_t* req, const aspd_branch_t* br
 
 static int plan_to_device(aspd_plan* p, cudaStream_t s);
 
-// Limits under which no logit overflows in fp32: a cap in log2 units, a slope times the largest distance.
-constexpr float kMostCap = 1e30f, kMostSlope = 1e30f;
-constexpr long kMostBiasPos = 1 << 24;      // position IDs are below that, so that their differences are exact in fp32
+// Limits: a cap in log2 units is an fp32 number; position IDs' differences are exact in fp32; and a bias is at most 2^29.6 in
+// log2 units, so that what is left of one after its reference (2^-24 of it at most) is no exponent that overflows.
+constexpr float kMostCap = 1e30f, kMostSlope = 32.f;
+constexpr long kMostBiasPos = 1 << 24;
 
 // like: the plan that this one is to take the place of (aspd_plan_update re-plans on the host for the device that
 // plan lives on): the grid of its device, its way of splitting the streams and, as far as possible, of writing new rows
@@ -688,7 +689,8 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
     // A step in which some request has more query tokens than one 128-row tile holds takes row blocks
     // of two tiles (the two-tile variant of the kernel: both tiles are scored against every K/V tile
     // the CTA fetches, one softmax group per tile), unless the caller asked for single tiles.
-    if (p->wide && tune.wide_rows != 128) {
+    // (capped scores: only with fixed references, which is what that kernel has for them)
+    if (p->wide && tune.wide_rows != 128 && (p->cap == 0.f || fixed_reference(p))) {
       int most_q = 0;
       for (const Block& bk : blocks) most_q = std::max(most_q, bk.n_tok);
       if (most_q > kMaxRowsWide / G || tune.wide_rows == 256) p->wide = 2;

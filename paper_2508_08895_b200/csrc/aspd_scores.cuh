@@ -11,22 +11,85 @@ namespace {
 
 struct ScoreParams {
   float scale;             // of the products, in log2 units
-  float cap_in, cap_out;   // 2 log2(e) sm_scale / cap and cap * log2(e); 0: scores are not capped
+  float cap_in, cap_out;   // sm_scale / cap and cap * log2(e); 0: scores are not capped
+  float poly[6];           // of cap * tanh(z) / z in z^2, |z| <= 1, log2 units
+  float poly_limit;        // products up to that magnitude have |z| <= 1
+  float near[4], near_limit;   // of cap * tanh(z) / product in the product's square, |z| <= 0.6, log2 units; up to that magnitude
 };
+// tanh(z) / z as a polynomial in z^2 of degree 5 on |z| <= 1 and of degree 3 on |z| <= 0.6, fitted for the least largest relative
+// error (Lawson's iteration of weighted least squares on Chebyshev points): 6.5e-7 and 2.3e-6 with their fp32 evaluation.
 inline ScoreParams score_params(const aspd_plan* p) {
   constexpr double kLog2E = 1.4426950408889634;
+  constexpr double kTanh[6] = {0.9999994039535522, -0.3332904279232025, 0.13281434774398804, -0.051605675369501114, 0.016743116080760956,
+                               -0.0030670601408928633};
+  constexpr double kTanhShort[4] = {0.9999978513027259, -0.33314039269087015, 0.1305785620279237, -0.04092942321980133};
   const double s = p->shape.sm_scale, c = p->cap;
-  return {(float)(s * kLog2E), c > 0 ? (float)(2 * kLog2E * s / c) : 0.f, (float)(c * kLog2E)};
+  ScoreParams sp = {(float)(s * kLog2E), 0.f, 0.f, {}, 0.f, {}, 0.f};
+  if (c > 0) {
+    sp.cap_in = (float)(s / c);
+    sp.cap_out = (float)(c * kLog2E);
+    sp.poly_limit = (float)(c / s);
+    for (int k = 0; k < 6; ++k) sp.poly[k] = (float)(kTanh[k] * c * kLog2E);
+    // the powers of sm_scale / cap in the coefficients: as far as they are ordinary fp32 numbers
+    const double z = s / c;
+    if (z > 1e-5 && z < 1e5) sp.near_limit = (float)(0.6 / z);
+    for (int k = 0; k < 4; ++k) sp.near[k] = sp.near_limit > 0.f ? (float)(kTanhShort[k] * s * kLog2E * pow(z, 2 * k)) : 0.f;
+  }
+  return sp;
 }
 
-// cap * tanh(x / cap) in log2 units, of a product: tanh(z) = 1 - 2 / (2^(2 z log2 e) + 1).  The exponential may overflow or
-// vanish: the ends are exact.  Off by about 2^-22 of the cap (near 0 the subtraction costs relative, not absolute precision, and a
-// logit's absolute error is what a weight sees): 1e-5 of a weight at a cap of 50.
-__device__ __forceinline__ float capped(float s, const ScoreParams& sp) {
+// cap * tanh(z), z = product * sm_scale / cap, in log2 units.  Up to |z| = 1 the polynomial; beyond, tanh|z| = 1 - 2 / (2^(2 |z|
+// log2 e) + 1), exact at its end (the exponential may overflow), off by 2^-22 of itself.  Either way a logit is off by less than 3e-6
+// of itself (7e-5 for a score of 30), far below what the rounding of queries and weights to bf16 does.
+//
+// saturated: the second form for any z, off by 2^-22 of the cap (near 0 its subtraction costs relative, not absolute, precision).
+__device__ __forceinline__ float saturated(float s, const ScoreParams& sp) {
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(s * sp.cap_in));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(s * sp.cap_in * 2.885390081777927f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
   return fmaf(-2.f * sp.cap_out, r, sp.cap_out);
+}
+__device__ __forceinline__ float capped(float s, const ScoreParams& sp) {
+  const float z = s * sp.cap_in, u = z * z;
+  float p = sp.poly[5], e, r;
+#pragma unroll
+  for (int k = 4; k >= 0; --k) p = fmaf(p, u, sp.poly[k]);
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(z) * 2.885390081777927f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
+  return fabsf(z) <= 1.f ? z * p : copysignf(fmaf(-2.f * sp.cap_out, r, sp.cap_out), z);
+}
+// N scores of a thread: where none passes |z| = 0.6, or 1, packed fp32 pairs and no special-function
+// unit, which the softmax's own exponentials keep busy already.  @MEASURED@
+template <int N>
+__device__ __forceinline__ void cap_scores(float (&s)[N], const ScoreParams& sp) {
+  float mx = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; i += 2) mx = fmaxf(mx, fmaxf(fabsf(s[i]), fabsf(s[i + 1])));
+  if (mx <= sp.near_limit) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 x = make_float2(s[i], s[i + 1]), u = __fmul2_rn(x, x);
+      float2 p = make_float2(sp.near[3], sp.near[3]);
+#pragma unroll
+      for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(sp.near[k], sp.near[k]));
+      p = __fmul2_rn(p, x);
+      s[i] = p.x; s[i + 1] = p.y;
+    }
+  } else if (mx <= sp.poly_limit) {
+    const float2 in = make_float2(sp.cap_in, sp.cap_in);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 z = __fmul2_rn(make_float2(s[i], s[i + 1]), in), u = __fmul2_rn(z, z);
+      float2 p = make_float2(sp.poly[5], sp.poly[5]);
+#pragma unroll
+      for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(sp.poly[k], sp.poly[k]));
+      p = __fmul2_rn(p, z);
+      s[i] = p.x; s[i + 1] = p.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = capped(s[i], sp);
+  }
 }
 
 // A query row's share of the distance bias
@@ -43,8 +106,7 @@ __device__ __forceinline__ RowBias row_bias(const PlanDevice& pd, int tok, int q
 template <int N>
 __device__ __forceinline__ void score_row(float (&s)[N], const ScoreParams& sp, bool biased, const RowBias& rb, const int* kpos) {
   if (sp.cap_in != 0.f) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = capped(s[i], sp);
+    cap_scores(s, sp);
   } else {
     const float2 sc = make_float2(sp.scale, sp.scale);
 #pragma unroll

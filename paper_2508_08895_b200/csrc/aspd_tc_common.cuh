@@ -202,6 +202,10 @@ __device__ __forceinline__ bool named_sync_or(int id, int n, bool pred) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, " \
                "%12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, "   \
                "%31};" ::ASPD_U32(v, o), "r"(taddr) : "memory")
+// 8 uint32 of this thread -> 8 consecutive columns of its TMEM lane
+#define ASPD_TMEM_ST8U(taddr, v)                                                                                  \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"                    \
+               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory")
 #define ASPD_TMEM_LD16(taddr, v, o)                                                                               \
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "  \
                "%13, %14, %15}, [%16];"                                                                          \
@@ -231,6 +235,9 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 // The same, with the 32 loaded values as its operands: nothing that uses them can be placed before it, while loads
 // issued after it may still be on their way.
 #define ASPD_RW8(v, o) "+f"(v[o + 0]), "+f"(v[o + 1]), "+f"(v[o + 2]), "+f"(v[o + 3]), "+f"(v[o + 4]), "+f"(v[o + 5]), "+f"(v[o + 6]), "+f"(v[o + 7])
+__device__ __forceinline__ void tmem_wait_ld16(float (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : ASPD_RW8(v, 0), ASPD_RW8(v, 8) :: "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld32(float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : ASPD_RW8(v, 0), ASPD_RW8(v, 8), ASPD_RW8(v, 16), ASPD_RW8(v, 24)::"memory");
 }
