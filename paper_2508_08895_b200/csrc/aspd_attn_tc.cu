@@ -152,7 +152,10 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
   return hi > lo ? ((0xFFFFu >> (16 - hi)) & ~((1u << lo) - 1u)) : 0u;
 }
 
-// SC: the plan's scores are capped or have a distance bias (score_row)
+// What the scores of a kernel instance's plans are: the plain products; capped or with a distance bias (score_row); capped with
+// fixed references (softmax_item_fixed).
+enum { kProducts = 0, kScored = 1, kFixed = 2 };
+
 template <int NC, bool SC>   // NC = padded row count R = columns of a row replica; a thread takes half of them
 __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p,
                                              uint32_t tmem, int item_no, int& g) {   // item_no = index among this CTA's items
@@ -351,6 +354,82 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
   // ---- hand the item's statistics to the epilogue warps and move on to the next item
   dead |= !mbar_wait(bars + 8 * (O_EMPTY + ob), ((item_no >> 1) & 1) ^ 1, ab);   // epilogue of item_no - 2 is done
   if (j == 0 && half == 0) misc->fin_m[ob][r] = m_ref;
+  misc->fin_l[ob][tid] = l;
+  mbar_arrive(bars + 8 * (E_FULL + ob));
+  return !named_sync_or(1, kSoftmaxThreads, dead || *ab);
+}
+
+// The same for capped scores with fixed references (aspd_plan::fixed_ref): no maximum, nothing exchanged, nothing taken twice, and the
+// scores' columns are free as soon as they are in registers.
+// @MEASURED@
+template <int NC>
+__device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p, uint32_t tmem,
+                                                   int item_no, int& g) {
+  constexpr int R = NC, HC = NC / 2;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5);
+  const int tmem_lane = tid & 127, half = tid >> 7;
+  const int r = tmem_lane % R, j = tmem_lane / R, col0 = j * NC + half * HC;      // as in softmax_item
+  const int G = c.G, M = it.n_q_tok * G, n_tiles = (it.n_pages + 7) >> 3;
+  volatile int* ab = &misc->abort_flag;
+  int4 vis = make_int4(0, 0, 0, 0);
+  RowBias rb = {0.f, 0};
+  const int tl = token_of(c, r);
+  const bool biased = c.pd.slopes != nullptr;
+  if (r < M) {
+    vis = (item_no < kItemCache && tl < kMaxTokPerItem) ? misc->vis[item_no][tl] : c.pd.tok_vis[it.q_tok0 + tl];
+    if (biased) rb = row_bias(c.pd, it.q_tok0 + tl, it.kv_head * G + r - tl * G);
+  }
+  const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+  const int ob = item_no & 1;
+  float l = 0.f;
+  bool dead = false;
+  for (int t = 0; t < n_tiles; ++t, ++g) {
+    const int sb = g & 1;
+    dead |= !mbar_wait(bars + 8 * (S_FULL + sb), (g >> 1) & 1, ab);
+    tc_fence_after();
+    float s[HC];
+    const uint32_t s_addr = tmem + lane_addr + COL_S + sb * 128 + col0;
+    if constexpr (HC == 32) { ASPD_TMEM_LD32(s_addr, s, 0); }
+    else { ASPD_TMEM_LD16(s_addr, s, 0); }
+    uint32_t mask[HC / 16];
+#pragma unroll
+    for (int pg = 0; pg < HC / 16; ++pg) {
+      const int ye = misc->nval[g & 3][col0 / 16 + pg], nv = ye & 255, kb = it.key0 + t * kTile + col0 + pg * 16;
+      mask[pg] = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb)) | bits_between(0, min(nv, vis.w - (ye >> 13) * 16));
+    }
+    if constexpr (HC == 32) tmem_wait_ld32(s);
+    else tmem_wait_ld16(s);
+    score_row(s, c.sp, biased, rb, &misc->kpos[g & 3][col0 / 16]);
+    tc_fence_before();
+    mbar_arrive(bars + 8 * (S_EMPTY + sb));       // the scores and the tile's entries are not needed again
+    float2 lsum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < HC; i += 2) {
+      float2 x = make_float2(s[i], s[i + 1]);
+      if (mask[i / 16] != 0xFFFFu) {
+        x.x = (mask[i / 16] >> (i & 15)) & 1u ? x.x : -INFINITY;
+        x.y = (mask[i / 16] >> ((i & 15) + 1)) & 1u ? x.y : -INFINITY;
+      }
+      x.x = ex2(x.x); x.y = ex2(x.y);
+      s[i] = x.x; s[i + 1] = x.y;
+      lsum = __fadd2_rn(lsum, x);
+    }
+    l += lsum.x + lsum.y;
+    if (g > 0) dead |= !mbar_wait(bars + 8 * P_EMPTY, (g - 1) & 1, ab);   // P tile is free again
+#pragma unroll
+    for (int c8 = 0; c8 < HC / 8; ++c8) {
+      const int kk = col0 + c8 * 8;
+      const uint32_t addr = smem_p + (kk >> 6) * kHalf + r * 128 + ((((kk & 63) >> 3) ^ (r & 7)) << 4);
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(pack_bf16(s[c8 * 8 + 0], s[c8 * 8 + 1])),
+                   "r"(pack_bf16(s[c8 * 8 + 2], s[c8 * 8 + 3])), "r"(pack_bf16(s[c8 * 8 + 4], s[c8 * 8 + 5])),
+                   "r"(pack_bf16(s[c8 * 8 + 6], s[c8 * 8 + 7])) : "memory");
+    }
+    fence_async_smem();
+    tc_fence_before();
+    mbar_arrive(bars + 8 * P_FULL);
+  }
+  dead |= !mbar_wait(bars + 8 * (O_EMPTY + ob), ((item_no >> 1) & 1) ^ 1, ab);   // epilogue of item_no - 2 is done
+  if (j == 0 && half == 0) misc->fin_m[ob][r] = 0.f;
   misc->fin_l[ob][tid] = l;
   mbar_arrive(bars + 8 * (E_FULL + ob));
   return !named_sync_or(1, kSoftmaxThreads, dead || *ab);
@@ -826,10 +905,10 @@ __device__ __forceinline__ bool patch_tile(uint32_t base, uint32_t bars, volatil
 //              narrow row blocks
 //   kPatch     kPlain for fused steps of plans that patch their tiles (patch_tile)
 enum { kPlain = 0, kOptions = 1, kPatch = 2 };
-// SC: instances for plans whose scores are not the plain products.
-template <bool WIDE, int MODE, bool SC>
+// SCORES: kProducts, kScored or kFixed.
+template <bool WIDE, int MODE, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
-  constexpr bool OPT = MODE == kOptions, PATCH = MODE == kPatch;
+  constexpr bool OPT = MODE == kOptions, PATCH = MODE == kPatch, SC = SCORES != kProducts;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -914,21 +993,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const DeviceItem it = get_item(c, misc, idx, item_begin);
       const int M = it.n_q_tok * c.G;
       bool ok;
-      if constexpr (WIDE) {
-        ok = M <= 32 ? softmax_item<32, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-           : M <= 64 ? softmax_item<64, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-                     : softmax_item_wide<SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
+      const uint32_t p = base + OFF_P;
+      if (WIDE && M > 64) {
+        if constexpr (WIDE) ok = softmax_item_wide<SC>(c, it, misc, bars, p, tmem, item_no, g);
+      } else if constexpr (SCORES == kFixed) {
+        ok = M <= 32 ? softmax_item_fixed<32>(c, it, misc, bars, p, tmem, item_no, g) : softmax_item_fixed<64>(c, it, misc, bars, p, tmem, item_no, g);
       } else {
         bool scores64 = false;                     // scores with M = 64 (plans with scores of their own never have them)
         if constexpr (OPT && !SC) {
           scores64 = c.m64;
           if (scores64)
-            ok = M <= 32 ? softmax_item_m64<32>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-                         : softmax_item_m64<64>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
+            ok = M <= 32 ? softmax_item_m64<32>(c, it, misc, bars, p, tmem, item_no, g) : softmax_item_m64<64>(c, it, misc, bars, p, tmem, item_no, g);
         }
         if (!scores64)
-          ok = M <= 32 ? softmax_item<32, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g)
-                       : softmax_item<64, SC>(c, it, misc, bars, base + OFF_P, tmem, item_no, g);
+          ok = M <= 32 ? softmax_item<32, SC>(c, it, misc, bars, p, tmem, item_no, g) : softmax_item<64, SC>(c, it, misc, bars, p, tmem, item_no, g);
       }
       if (!ok) break;
     }
@@ -1321,12 +1399,13 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
     auto attr = [](auto* kernel, size_t bytes) {
       return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
     };
-    auto all = [&](auto sc) {
-      constexpr bool SC = decltype(sc)::value;
-      return attr(attn_tc_kernel<false, kPlain, SC>, kSmemBytes) && attr(attn_tc_kernel<false, kOptions, SC>, kSmemBytes) &&
-             attr(attn_tc_kernel<false, kPatch, SC>, kSmemBytes) && attr(attn_tc_kernel<true, kPlain, SC>, kSmemBytes);
+    auto all = [&](auto scores) {
+      constexpr int S = decltype(scores)::value;
+      return attr(attn_tc_kernel<false, kPlain, S>, kSmemBytes) && attr(attn_tc_kernel<false, kOptions, S>, kSmemBytes) &&
+             attr(attn_tc_kernel<false, kPatch, S>, kSmemBytes) && attr(attn_tc_kernel<true, kPlain, S>, kSmemBytes);
     };
-    if (!all(std::false_type()) || !all(std::true_type()) || !attr(attn_tc_w2_kernel<kPlainScores>, kSmemBytesW2) ||
+    if (!all(std::integral_constant<int, kProducts>()) || !all(std::integral_constant<int, kScored>()) ||
+        !all(std::integral_constant<int, kFixed>()) || !attr(attn_tc_w2_kernel<kPlainScores>, kSmemBytesW2) ||
         !attr(attn_tc_w2_kernel<kCapped>, kSmemBytesW2) || !attr(attn_tc_w2_kernel<kBiased>, kSmemBytesW2) ||
         !attr(attn_tc_w2_kernel<kCapped | kBiased>, kSmemBytesW2))
       return ASPD_ERR_CUDA;
@@ -1367,13 +1446,14 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
                             : (biased ? attn_tc_w2_kernel<kBiased> : attn_tc_w2_kernel<kPlainScores>);
     return launch_pdl(w2, dim3(p->n_ctas), dim3(kThreadsW2), kSmemBytesW2, s, c) == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
   }
-  auto instance = [&](auto sc) {
-    constexpr bool SC = decltype(sc)::value;
-    return p->wide ? attn_tc_kernel<true, kPlain, SC>
-           : c.m64 || c.merge_out != nullptr || c.out != nullptr ? attn_tc_kernel<false, kOptions, SC>
-           : c.k_new != nullptr && p->patch_tiles ? attn_tc_kernel<false, kPatch, SC> : attn_tc_kernel<false, kPlain, SC>;
+  auto instance = [&](auto scores) {
+    constexpr int S = decltype(scores)::value;
+    return p->wide ? attn_tc_kernel<true, kPlain, S>
+           : c.m64 || c.merge_out != nullptr || c.out != nullptr ? attn_tc_kernel<false, kOptions, S>
+           : c.k_new != nullptr && p->patch_tiles ? attn_tc_kernel<false, kPatch, S> : attn_tc_kernel<false, kPlain, S>;
   };
-  auto* kernel = p->scored() ? instance(std::true_type()) : instance(std::false_type());
+  auto* kernel = !p->scored() ? instance(std::integral_constant<int, kProducts>())
+                 : p->fixed_ref ? instance(std::integral_constant<int, kFixed>()) : instance(std::integral_constant<int, kScored>());
   const cudaError_t e = launch_pdl(kernel, dim3(p->n_ctas), dim3(kThreads), kSmemBytes, s, c);
   return e == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
 }

@@ -172,7 +172,7 @@ __device__ __forceinline__ float far_half(const Ctx& c, const MiscW2* misc, cons
 }
 
 // One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.
-// SC: kCapped | kBiased.  Capped scores come here only with fixed references (fixed_reference): the exponentials are taken against 0
+// SC: kCapped | kBiased.  Capped scores come here only with fixed references (aspd_plan::fixed_ref): the exponentials are taken against 0
 // always.  A half is one pass with the short polynomial, which keeps the largest product; where that turns out to be beyond the
 // polynomial's range (scores above 0.6 of the cap) the half is taken again by far_half, and the warp's next half goes there at once.
 template <int SC>

@@ -14,6 +14,10 @@ namespace aspd {
 constexpr int kMaxRowsPerItem = 64;   // query rows (tokens x group heads) one work item carries
 constexpr int kMaxRowsWide = 128;     // ... in a plan that deals whole streams to the tensor-core kernel's CTAs
 constexpr int kMostFusedRows = 20;   // new rows per CTA up to which the attention pass writes them itself (short CTAs; long ones write any number)
+// Softmax weights of a capped row need no maximum: its logits lie within +-cap, a bias with slopes of 0 and more and no key later
+// than its query only lowers them, and the row's own key, at distance 0, is not lowered at all.  Up to this cap in log2 units (scores up
+// to 55) weights taken against 0 neither overflow in sums over 2^24 keys times values of 2^20, nor vanish where they matter.
+constexpr float kFixedCap = 80.f;
 constexpr int kCausalAll = 1 << 29;   // prefix end of a token that sees its whole key stream
 
 // ---------------------------------------------------------------------------------------
@@ -140,6 +144,7 @@ struct aspd_plan {
   int single_launch = 0;           // stream-K plan of the tensor-core kernel whose last-arriving CTAs merge the records themselves
   float cap = 0.f;                 // scores are capped (0: not)
   int rotated = 0;                 // q and k_new come rotated
+  int fixed_ref = 0;               // capped scores whose softmax weights are taken against 0 always (see kFixedCap)
   std::vector<float> slopes;       // distance bias per query head (empty: none)
   std::vector<int32_t> page_pos, bias_pos;   // with slopes: see PlanDevice
   bool scored() const { return cap > 0.f || !slopes.empty(); }   // the scores are not the plain products
@@ -234,15 +239,6 @@ inline void fill_cta_head(const aspd_plan* p, int4* dst) {
     dst[2 * c] = make_int4(b, e, b < e ? p->items[b].page0 : 0, b < e ? p->items[b].n_pages : 0);
     dst[2 * c + 1] = make_int4(p->cta_dirty0[c], p->cta_dirty0[c + 1] - p->cta_dirty0[c], 0, 0);
   }
-}
-// Softmax weights of a capped row need no maximum: its logits lie within +-cap, a bias with slopes of 0 and more only lowers them, and
-// the row's own key, at distance 0, is not lowered at all.  Up to this cap in log2 units (scores up to 55) weights taken against 0
-// neither overflow in sums over 2^24 keys times values of 2^20, nor vanish where they matter.
-constexpr float kFixedCap = 80.f;
-inline bool fixed_reference(const aspd_plan* p) {
-  bool falling = true;
-  for (float s : p->slopes) falling = falling && s >= 0.f;
-  return p->cap > 0.f && p->cap * 1.4426950408889634f <= kFixedCap && falling;
 }
 // the device plan's slopes, from the host's
 inline void fill_slopes(const aspd_plan* p, float* dst) {

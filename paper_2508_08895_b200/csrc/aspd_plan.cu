@@ -1,6 +1,7 @@
 // Host side of the library: descriptor validation, position IDs and slots (integer rules of
 // Eq. 4 and Section 3.3), the split-K work list, plan life cycle and the C entry points.
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -473,16 +474,23 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
       if (br[q.branch_begin + b].q_len == ASPD_Q_SHARED) s += br[q.branch_begin + b].kv_len;
     return s;
   };
-  for (int r = 0; biased && r < n_req; ++r) {
-    long total = req[r].prefix_len;
+  bool falling = true;                                // the bias raises no logit
+  for (int h = 0; biased && h < Hq; ++h) falling = falling && scores->slopes[h] >= 0.f;
+  for (int r = 0, t = 0; biased && r < n_req; ++r) {
+    long total = req[r].prefix_len, last_seen = req[r].prefix_len - 1, first_query = LONG_MAX;   // of keys outside a query's own branch; position IDs
+    for (; t < n_new && treq[t] == r; ++t) first_query = std::min<long>(first_query, p->bias_pos[t]);
     for (int b = 0; b < req[r].n_branches; ++b) {
       const aspd_branch_t& x = br[req[r].branch_begin + b];
       if (x.kv_len > 0 && x.q_len == ASPD_Q_SHARED && x.pos_start == ASPD_POS_AUTO) { delete p; return ASPD_ERR_BAD_DESCRIPTOR; }
       if (region_start(req[r], x) + x.kv_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
+      if (x.kv_len > 0 && (mode == ASPD_MODE_SERIAL || x.q_len == ASPD_Q_SHARED)) last_seen = std::max(last_seen, region_start(req[r], x) + x.kv_len - 1);
+      if (shared_mask && x.q_len >= 0) falling = falling && region_start(req[r], x) == region_start(req[r], br[req[r].branch_begin]);
       total += x.kv_len;
     }
     if (total + req[r].tail_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
+    falling = falling && last_seen <= first_query;
   }
+  p->fixed_ref = (cap > 0.f && cap * 1.4426950408889634f <= kFixedCap && falling) ? 1 : 0;
   std::vector<int4> tok_vis(n_new);
   int64_t kv_tokens = 0;
   const bool tok_field_fits = n_new < (1 << 18);      // the 18 bits above bit 13 of a page entry hold a token index
@@ -690,7 +698,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
     // of two tiles (the two-tile variant of the kernel: both tiles are scored against every K/V tile
     // the CTA fetches, one softmax group per tile), unless the caller asked for single tiles.
     // (capped scores: only with fixed references, which is what that kernel has for them)
-    if (p->wide && tune.wide_rows != 128 && (p->cap == 0.f || fixed_reference(p))) {
+    if (p->wide && tune.wide_rows != 128 && (p->cap == 0.f || p->fixed_ref)) {
       int most_q = 0;
       for (const Block& bk : blocks) most_q = std::max(most_q, bk.n_tok);
       if (most_q > kMaxRowsWide / G || tune.wide_rows == 256) p->wide = 2;
@@ -1187,7 +1195,7 @@ int aspd_plan_update(aspd_plan_t* p, const aspd_request_t* req, const aspd_branc
   if (rc) return rc;
   const aspd::PlanLayout& L = p->layout;
   if (t->n_new != p->n_new || t->n_ctas != p->n_ctas || t->base_ctas != p->base_ctas || t->kernel != p->kernel || t->wide != p->wide || t->dealt != p->dealt ||
-      t->fuse_append != p->fuse_append || t->shared_mask != p->shared_mask || t->single_launch != p->single_launch || t->m64 != p->m64 || (p->dec && padded_rows(t->max_rows) != padded_rows(p->max_rows)) || t->kernel != ASPD_KERNEL_MMA ||
+      t->fuse_append != p->fuse_append || t->shared_mask != p->shared_mask || t->fixed_ref != p->fixed_ref || t->single_launch != p->single_launch || t->m64 != p->m64 || (p->dec && padded_rows(t->max_rows) != padded_rows(p->max_rows)) || t->kernel != ASPD_KERNEL_MMA ||
       t->row_blocks.size() != L.n_row_blocks || t->part_base.size() != L.n_part_base) {
     delete t;
     return ASPD_ERR_UNSUPPORTED;
