@@ -62,7 +62,8 @@ struct DecMisc {
   int abort_flag;
 };
 
-// What the instances for plans with scores of their own keep behind it
+// What the instances for plans with scores of their own keep behind it (rows' slopes and positions are read four at a time)
+static_assert(sizeof(DecMisc) % 16 == 0, "ScoreMisc lies on a 16-byte boundary");
 struct ScoreMisc {
   int kpos[2 * kMaxSlots][16];  // position IDs of the pages' first rows (ring as nval)
   float slope[2][64], pos[2][64];   // per query row, by item parity: slope, position ID of its token
@@ -270,6 +271,27 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
   if (lane == 0) mbar_arrive(bar);
 }
 
+// Key kl's weights of rows r0 ... as its row of P^T: NR bf16, 16-byte chunks swizzled over the atom's width, in pieces
+template <int NR>
+__device__ __forceinline__ void store_p(float (&s)[NR / 2], uint32_t smem_p, int kl, int r0) {
+  const int sw = NR == 64 ? kl & 7 : NR == 32 ? (kl >> 1) & 3 : (kl >> 2) & 1;
+#pragma unroll
+  for (int c8 = 0; c8 < NR / 16; ++c8) {
+    const uint32_t addr = smem_p + kl * (NR * 2) + (((r0 / 8 + c8) ^ sw) << 4);
+    uint32_t w[4];
+#pragma unroll
+    for (int pc = 0; pc < kPieces; ++pc) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float &x = s[c8 * 8 + 2 * i], &y = s[c8 * 8 + 2 * i + 1];
+        w[i] = pc == 0 ? pack_bf16(x, y) : pack_next(x, y, w[i]);
+      }
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + pc * (kTile * NR * 2)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                   : "memory");
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------- softmax of an item
 // All tiles of one item: scores out of tensor memory, exponentials, P^T.  Leaves the row sums of every quadrant's
 // keys in misc->wm.
@@ -400,23 +422,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
 #pragma unroll
     for (int i = 0; i < HC / 2; ++i) l2[i] = __fadd2_rn(l2[i], make_float2(s[2 * i], s[2 * i + 1]));
     if (g > 0) dead |= !mbar_wait(bars + 8 * P_EMPTY, (g - 1) & 1, ab);   // the P^T tile is free again
-    // key kl's row of P^T: NR bf16, 16-byte chunks swizzled over the atom's width
-    const int sw = NR == 64 ? kl & 7 : NR == 32 ? (kl >> 1) & 3 : (kl >> 2) & 1;
-#pragma unroll
-    for (int c8 = 0; c8 < HC / 8; ++c8) {
-      const uint32_t addr = smem_p + kl * (NR * 2) + (((r0 / 8 + c8) ^ sw) << 4);
-      uint32_t w[4];
-#pragma unroll
-      for (int pc = 0; pc < kPieces; ++pc) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float &x = s[c8 * 8 + 2 * i], &y = s[c8 * 8 + 2 * i + 1];
-          w[i] = pc == 0 ? pack_bf16(x, y) : pack_next(x, y, w[i]);
-        }
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + pc * (kTile * NR * 2)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                     : "memory");
-      }
-    }
+    store_p<NR>(s, smem_p, kl, r0);
     fence_async_smem();
     tc_fence_before();
     warp_arrive(bars + 8 * P_FULL, lane);
@@ -427,6 +433,81 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
   const float sum = lane_reduce<HC>(l, lane, [](float a, float b) { return a + b; });
   constexpr int REP = 32 / HC;
   if (lane % REP == 0) misc->wm[q][r0 + lane / REP] = sum;
+  return !dead;
+}
+
+// The same for capped scores with fixed references (aspd_plan::fixed_ref): no maximum, no barrier, nothing taken twice.
+// @MEASURED@
+template <int D, int NR>
+__device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceItem& it, DecMisc* misc, uint32_t bars, uint32_t smem_p, uint32_t tmem,
+                                                   int par, int& g) {
+  constexpr int HC = NR / 2;
+  const ScoreMisc* sm = reinterpret_cast<const ScoreMisc*>(misc + 1);
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, q = warp & 3, r0 = (warp >> 2) * HC;
+  const int kl = q * 32 + lane;                                  // this thread's key inside a tile
+  const int ps = c.page_size, ps_shift = 31 - __clz(ps), ppt = kTile >> ps_shift;
+  const int G = c.n_q_heads / c.n_kv_heads;
+  const int n_tiles = (it.n_pages + ppt - 1) / ppt, pe = misc->vis[par][0].x;
+  const bool biased = c.pd.slopes != nullptr;
+  volatile int* ab = &misc->abort_flag;
+  const uint32_t lane_addr = (uint32_t)(q * 32) << 16;
+  float2 l2[HC / 2];
+#pragma unroll
+  for (int i = 0; i < HC / 2; ++i) l2[i] = make_float2(0.f, 0.f);
+  bool dead = false;
+  for (int t = 0; t < n_tiles; ++t, ++g) {
+    const int sb = g & 1, ring = g & (2 * kMaxSlots - 1);
+    dead |= !mbar_wait(bars + 8 * (S_FULL + sb), (g >> 1) & 1, ab);
+    tc_fence_after();
+    float s[HC];
+    tmem_ld<HC>(tmem + lane_addr + COL_S + sb * 64 + r0, s);
+    const int ye = misc->nval[ring][kl >> ps_shift], row = kl & (ps - 1), kg = it.key0 + t * kTile + kl;
+    const float kp = biased ? (float)(sm->kpos[ring][kl >> ps_shift] + row) : 0.f;
+    const bool valid = row < (ye & 255), full = __all_sync(0xffffffffu, valid && kg < pe) != 0;
+    uint32_t bits = 0xffffffffu;
+    if (!full) {
+      bits = 0;
+      const int ofs = (ye >> 13) * ps + row;
+      for (int tl = r0 / G; tl < it.n_q_tok && tl * G < r0 + HC; ++tl) {
+        const int4 v = misc->vis[par][tl];
+        const int a = max(tl * G - r0, 0), b = min(tl * G + G - r0, HC);
+        if (valid && (kg < v.x || (kg >= v.y && kg < v.z) || ofs < v.w)) bits |= (0xffffffffu >> (32 - b)) & ~((1u << a) - 1u);
+      }
+    }
+    tmem_wait_ld();
+    tc_fence_before();
+    warp_arrive(bars + 8 * (S_EMPTY + sb), lane);                 // the scores are in registers, the tile's entries read
+    cap_scores(s, c.sp);
+#pragma unroll
+    for (int i = 0; i < HC; i += 4) {
+      float2 x0 = make_float2(s[i], s[i + 1]), x1 = make_float2(s[i + 2], s[i + 3]);
+      if (biased) {
+        const float4 sl = *reinterpret_cast<const float4*>(&sm->slope[par][r0 + i]), qp = *reinterpret_cast<const float4*>(&sm->pos[par][r0 + i]);
+        x0 = __ffma2_rn(make_float2(sl.x, sl.y), make_float2(kp - qp.x, kp - qp.y), x0);
+        x1 = __ffma2_rn(make_float2(sl.z, sl.w), make_float2(kp - qp.z, kp - qp.w), x1);
+      }
+      if (!full) {
+        x0.x = (bits >> i) & 1u ? x0.x : -INFINITY;       x0.y = (bits >> (i + 1)) & 1u ? x0.y : -INFINITY;
+        x1.x = (bits >> (i + 2)) & 1u ? x1.x : -INFINITY; x1.y = (bits >> (i + 3)) & 1u ? x1.y : -INFINITY;
+      }
+      x0.x = ex2(x0.x); x0.y = ex2(x0.y); x1.x = ex2(x1.x); x1.y = ex2(x1.y);
+      s[i] = x0.x; s[i + 1] = x0.y; s[i + 2] = x1.x; s[i + 3] = x1.y;
+      l2[i / 2] = __fadd2_rn(l2[i / 2], x0);
+      l2[i / 2 + 1] = __fadd2_rn(l2[i / 2 + 1], x1);
+    }
+    if (g > 0) dead |= !mbar_wait(bars + 8 * P_EMPTY, (g - 1) & 1, ab);   // the P^T tile is free again
+    store_p<NR>(s, smem_p, kl, r0);
+    fence_async_smem();
+    tc_fence_before();
+    warp_arrive(bars + 8 * P_FULL, lane);
+  }
+  float l[HC];
+#pragma unroll
+  for (int i = 0; i < HC / 2; ++i) { l[2 * i] = l2[i].x; l[2 * i + 1] = l2[i].y; }
+  const float sum = lane_reduce<HC>(l, lane, [](float a, float b) { return a + b; });
+  constexpr int REP = 32 / HC;
+  if (lane % REP == 0) misc->wm[q][r0 + lane / REP] = sum;
+  if (tid < NR) misc->ref[tid] = 0.f;
   return !dead;
 }
 
@@ -571,8 +652,11 @@ __device__ __noinline__ void redo_item(const Ctx& c, const DeviceItem it, DecMis
 // NR: rows that the plan's largest row block is padded to; its smaller blocks are padded as far.  (One instance that
 // chose per item was 161 KB of code, these are 65 to 99, and a short launch waits for its instructions: 14.5 against
 // 14.1 us a layer in a graph on the step above.)
-template <int D, int NR, bool SC>
+// SCORES: the plain products; capped or with a distance bias; capped with fixed references.
+enum { kProducts = 0, kScored = 1, kFixed = 2 };
+template <int D, int NR, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_constant__ Ctx c) {
+  constexpr bool SC = SCORES != kProducts;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   DecMisc* misc = reinterpret_cast<DecMisc*>(smem_raw + (base - raw) + c.off_misc);
@@ -644,7 +728,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dec_kernel(const __grid_cons
       const DeviceItem it = idx == item_begin ? first : uniform_item(c.pd.items[idx]);
       const int par = item_no & 1;
       named_sync(1, kSmThreads);                                  // the item's ranges are there
-      dead |= !softmax_item<D, NR, SC>(c, it, misc, bars, base + c.off_p, tmem, par, g);
+      if constexpr (SCORES == kFixed) dead |= !softmax_item_fixed<D, NR>(c, it, misc, bars, base + c.off_p, tmem, par, g);
+      else dead |= !softmax_item<D, NR, SC>(c, it, misc, bars, base + c.off_p, tmem, par, g);
       if (idx + 1 < item_end) {                                   // the next query tile as soon as this item's last scores are issued
         dead |= !mbar_wait(bars + 8 * Q_EMPTY, item_no & 1, ab);
         start_item(uniform_item(c.pd.items[idx + 1]), par ^ 1);
@@ -813,23 +898,23 @@ inline uint32_t smem_layout(int D, int nr, bool scored, Ctx* c) {
   return c->off_misc + misc + 1024;
 }
 
-template <int D, int NR, bool SC>
+template <int D, int NR, int SCORES>
 cudaError_t launch_instance(const aspd_plan* p, Ctx& c, cudaStream_t s) {
   static bool configured[64] = {};                 // the attribute belongs to the (function, device) pair
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(attn_dec_kernel<D, NR, SC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
+    e = cudaFuncSetAttribute(attn_dec_kernel<D, NR, SCORES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  const uint32_t smem = smem_layout(D, NR, SC, &c);
-  return launch_pdl(attn_dec_kernel<D, NR, SC>, dim3(p->n_ctas), dim3(kThreads), smem, s, c);
+  const uint32_t smem = smem_layout(D, NR, SCORES != kProducts, &c);
+  return launch_pdl(attn_dec_kernel<D, NR, SCORES>, dim3(p->n_ctas), dim3(kThreads), smem, s, c);
 }
 template <int D, int NR>
 cudaError_t launch(const aspd_plan* p, Ctx& c, cudaStream_t s) {
-  return p->scored() ? launch_instance<D, NR, true>(p, c, s) : launch_instance<D, NR, false>(p, c, s);
+  return !p->scored() ? launch_instance<D, NR, kProducts>(p, c, s) : p->fixed_ref ? launch_instance<D, NR, kFixed>(p, c, s) : launch_instance<D, NR, kScored>(p, c, s);
 }
 
 }  // namespace
