@@ -1444,7 +1444,7 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
     if (p->cap == 0.f) c.scale_log2 = c.sp.scale;      // (this kernel's instances without a cap scale as the plain one does)
     auto* w2 = p->cap > 0.f ? (biased ? attn_tc_w2_kernel<kCapped | kBiased> : attn_tc_w2_kernel<kCapped>)
                             : (biased ? attn_tc_w2_kernel<kBiased> : attn_tc_w2_kernel<kPlainScores>);
-    return launch_pdl(w2, dim3(p->n_ctas), dim3(kThreadsW2), kSmemBytesW2, s, c) == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
+    return launch_pdl(w2, dim3(p->n_ctas), dim3(p->cap > 0.f ? kThreadsW2<kCapped> : kThreadsW2<kPlainScores>), kSmemBytesW2, s, c) == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
   }
   auto instance = [&](auto scores) {
     constexpr int S = decltype(scores)::value;

@@ -33,8 +33,10 @@
 
 namespace {      // included inside namespace aspd
 
-constexpr int kThreadsW2 = 384;               // 168 registers a thread; 44 bytes are spilled
-constexpr int W2_KPROD = 8, W2_VPROD = 9, W2_ISSUE = 10;
+// What a plan's scores are, beside the plain products (see aspd_scores.cuh); an instance of the kernel for each.
+enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
+template <int SCORES> constexpr int kSoftmaxWarpsW2 = SCORES & kCapped ? 16 : 8;
+template <int SCORES> constexpr int kThreadsW2 = (kSoftmaxWarpsW2<SCORES> + 4) * 32;   // 384: 168 registers a thread; 44 bytes are spilled.  640: 96
 constexpr uint32_t W2_OFF_K = 0, W2_OFF_V = 2 * kTileBytes, W2_OFF_Q = 4 * kTileBytes, W2_OFF_OUT = 6 * kTileBytes,
                    W2_OFF_MISC = 7 * kTileBytes;
 constexpr size_t kSmemBytesW2 = 7 * kTileBytes + 2048 + 1024;   // + Misc + slack to align the base to 1024
@@ -73,15 +75,17 @@ __device__ __forceinline__ void warp_arrive_w2(uint32_t bar) {
 
 // The group's query tile of an item: rows rotated (RoPE at the token's position, cos/sin table of the plan), bf16,
 // as the 128-byte-swizzled K-major A operand (rows beyond the item's are zero).  A thread takes the 16-byte chunk
-// `rank % 8` of both halves of rows rank / 8 + 16 u; all of its query loads are on their way before the first is used.
+// `rank % 8` of both halves of rows rank / 8 + NT / 8 u; all of its query loads are on their way before the first is used.
+template <int NT>
 __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok, int kv_head, uint32_t qbuf, int rank) {
   const int G = c.G, M = n_tok * G, ch = rank & 7, row0 = rank >> 3;
   const __nv_bfloat16* q0 = c.q + ((size_t)q_tok0 * c.n_q_heads + kv_head * G) * 128 + ch * 8;
   const float4* cs0 = reinterpret_cast<const float4*>(c.pd.q_cs + (size_t)q_tok0 * 64 + ch * 8);
-  uint4 a[8], b[8];
+  constexpr int STEP = NT / 8, U = 128 / STEP;
+  uint4 a[U], b[U];
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const int r = row0 + 16 * u, tl = token_of(c, r);
+  for (int u = 0; u < U; ++u) {
+    const int r = row0 + STEP * u, tl = token_of(c, r);
     a[u] = make_uint4(0, 0, 0, 0); b[u] = make_uint4(0, 0, 0, 0);
     if (r < M) {
       const __nv_bfloat16* p = q0 + (size_t)(tl * (c.n_q_heads - G) + r) * 128;      // (tl * n_q_heads + r - tl * G) rows further
@@ -90,8 +94,8 @@ __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok
     }
   }
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const int r = row0 + 16 * u, tl = token_of(c, r);
+  for (int u = 0; u < U; ++u) {
+    const int r = row0 + STEP * u, tl = token_of(c, r);
     const float4* cs = cs0 + (size_t)(r < M ? tl : 0) * 32;
     const __nv_bfloat162* a2 = reinterpret_cast<const __nv_bfloat162*>(&a[u]);
     const __nv_bfloat162* b2 = reinterpret_cast<const __nv_bfloat162*>(&b[u]);
@@ -110,9 +114,7 @@ __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok
   fence_async_smem();
 }
 
-// What a plan's scores are, beside the plain products (see aspd_scores.cuh); an instance of the kernel for each.
-enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
-
+// One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.
 // A half whose scores reach beyond the short polynomial, 16 at a time out of tensor memory and their P back over scores that have
 // been read (P of scores 16 i ... takes columns 8 i ...): the longer polynomial up to the cap, two more special functions a score
 // beyond.  Returned: the row's sum.  A loop, and a short one, on purpose: the passes are straight code, and forms of
@@ -175,7 +177,7 @@ __device__ __forceinline__ float far_half(const Ctx& c, const MiscW2* misc, cons
 // SC: kCapped | kBiased.  Capped scores come here only with fixed references (aspd_plan::fixed_ref): the exponentials are taken against 0
 // always.  A half is one pass with the short polynomial, which keeps the largest product; where that turns out to be beyond the
 // polynomial's range (scores above 0.6 of the cap) the half is taken again by far_half, and the warp's next half goes there at once.
-template <int SC>
+template <bool BIAS>
 __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                  int item_end, int grp, int tpt) {
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, r = tid & 127;
@@ -191,7 +193,7 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
     for (; idx < item_end; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
       if (it.n_q_tok > grp * tpt) {
-        prep_tile_w2(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, r);
+        prep_tile_w2<128>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, r);
         warp_arrive_w2(bar_qfull);
         break;
       }
@@ -209,10 +211,8 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
     const int tl = token_of(c, r), M = n_tok * G, tok = it.q_tok0 + grp * tpt + tl;
     int4 vis = make_int4(0, 0, 0, 0);                          // padding rows see nothing
     if (r < M) vis = c.pd.tok_vis[tok];
-    constexpr bool CAP = SC & kCapped, BIAS = SC & kBiased;
     RowBias rb = {0.f, 0};
     if (BIAS && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
-    bool far = false;                                           // the warp's last half had scores beyond the short polynomial
     float m_ref = 0.f, l = 0.f;                                 // see the one-tile variant: the reference starts at 0
     bool seen = r >= M;                                         // padding rows never need the tracking pass
     bool warp_seen = false;                                     // all rows of the warp have (kept up in the full path only)
@@ -247,30 +247,11 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
         // then (and for rows that have not seen a key yet) finds the maximum.
         const int kb0 = kbt + h * 64;
         const bool masked = h ? masked1 : masked0;
-        float top;                                  // capped: largest product
-        // KIND: exponents against a reference and their largest (kTracked) or not (kPlainPass); kNear: capped
-        enum { kPlainPass, kTracked, kNear };
-        auto pass_impl = [&](float ref, auto kind_tag, auto masked_tag) {
-          constexpr int KIND = decltype(kind_tag)::value;
-          constexpr bool TRACK = KIND == kTracked, MASKED = decltype(masked_tag)::value;
-          if (CAP) top = 0.f;
+        auto pass_impl = [&](float ref, auto track_tag, auto masked_tag) {
+          constexpr bool TRACK = decltype(track_tag)::value, MASKED = decltype(masked_tag)::value;
           float mx0 = -INFINITY, mx1 = -INFINITY;
           float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0, sum2 = sum0, sum3 = sum0;
           const float2 sc2 = make_float2(c.scale_log2, c.scale_log2), nb2 = make_float2(-ref, -ref), sl2 = make_float2(rb.slope, rb.slope);
-          // logits less the reference
-          auto exponents = [&](float a, float b, float2 less) {
-            const float2 x = make_float2(a, b);
-            if constexpr (KIND == kNear) {
-              top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
-              const float2 u = __fmul2_rn(x, x);
-              float2 p = make_float2(c.sp.near[3], c.sp.near[3]);
-#pragma unroll
-              for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.near[k], c.sp.near[k]));
-              return __ffma2_rn(x, p, less);
-            } else {
-              return __ffma2_rn(x, sc2, less);
-            }
-          };
           float s0[32], s1[32];
           ASPD_TMEM_LD32(s_base + h * 64, s0, 0);
           tmem_wait_ld32(s0);
@@ -303,8 +284,8 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
               };
 #pragma unroll
               for (int i = 0; i < 16; i += 4) {
-                float2 x0 = exponents(s[pg * 16 + i], s[pg * 16 + i + 1], less());
-                float2 x1 = exponents(s[pg * 16 + i + 2], s[pg * 16 + i + 3], less());
+                float2 x0 = __ffma2_rn(make_float2(s[pg * 16 + i], s[pg * 16 + i + 1]), sc2, less());
+                float2 x1 = __ffma2_rn(make_float2(s[pg * 16 + i + 2], s[pg * 16 + i + 3]), sc2, less());
                 if (MASKED && mask != 0xFFFFu) {
                   x0.x = (mask >> i) & 1u ? x0.x : -INFINITY;
                   x0.y = (mask >> (i + 1)) & 1u ? x0.y : -INFINITY;
@@ -324,34 +305,20 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
           tile_sum = st.x + st.y;
           tmax = fmaxf(mx0, mx1);
         };
-        if constexpr (CAP) {
-          bool again = far;
-          if (!again) {
-            if (masked) pass_impl(0.f, std::integral_constant<int, kNear>(), std::true_type());
-            else pass_impl(0.f, std::integral_constant<int, kNear>(), std::false_type());
-            again = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
-          }
-          if (again) {
-            tile_sum = far_half<BIAS>(c, misc, rb, vis, s_base + h * 64, g & (kPageRingW2 - 1), 4 * h, kb0, top);
-            far = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
-          } else {
-            ASPD_TMEM_ST32U(s_base + h * 64, pk, 0);
-          }
-        } else {
-        auto pass = [&](float ref, auto kind_tag) {
-          if (masked) pass_impl(ref, kind_tag, std::true_type());
-          else pass_impl(ref, kind_tag, std::false_type());
+        auto pass = [&](float ref, auto track_tag) {
+          if (masked) pass_impl(ref, track_tag, std::true_type());
+          else pass_impl(ref, track_tag, std::false_type());
         };
         // The common case -- every row of the warp has seen a key and no exponent passed 2^40 -- is
         // the plain pass and one vote; everything else goes the full way.
         bool settled = false;
         if (warp_seen) {
-          pass(m_ref, std::integral_constant<int, kPlainPass>());
+          pass(m_ref, std::false_type());
           // an exponent beyond 2^40 makes the sum exceed it (the converse is harmless: one more pass)
           settled = !__any_sync(0xffffffffu, !(tile_sum <= kRaiseSumW2));
         }
         if (!settled) {
-          pass(m_ref, std::integral_constant<int, kTracked>());
+          pass(m_ref, std::true_type());
           // move the reference: up when an exponent passed 2^40; down only while the row has not seen a
           // key yet (l and its row of O are still exactly 0 then, so nothing is rescaled)
           const bool raise = tmax > kRaiseW2, lower = !seen && tmax < -kLower && tmax > -INFINITY;
@@ -377,15 +344,14 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
               }
               tmem_wait_st();
             }
-            pass(m_ref, std::integral_constant<int, kPlainPass>());           // the whole warp again (TMEM loads are warp-wide)
+            pass(m_ref, std::false_type());           // the whole warp again (TMEM loads are warp-wide)
           }
-        }
-        ASPD_TMEM_ST32U(s_base + h * 64, pk, 0);
         }
         l += tile_sum;
         if (tid == 0) ASPD_STAMP(c, g, 4 * h + 1);
-        // (the half's P, 64 bf16 = 32 columns, lies over its own scores, which nobody needs any more: the next
-        // scores go there behind the P.V that reads it, from the same issuer)
+        // the half's P (64 bf16 = 32 columns) over its own scores, which nobody needs any more: the next
+        // scores go there behind the P.V that reads it, from the same issuer
+        ASPD_TMEM_ST32U(s_base + h * 64, pk, 0);
         tmem_wait_st();
         tc_fence_before();
         warp_arrive_w2(bar_pfull + 8 * h);
@@ -436,8 +402,229 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 }
 
 
+// A thread's 32 scores of a half that reach beyond the short polynomial, 16 at a time out of tensor memory and their P back over scores
+// that have been read (P of scores 16 i ... takes columns 8 i ...): the longer polynomial up to the cap, two more special functions a score
+// beyond.  Returned: the row's sum.  A loop, and a short one, on purpose: the passes are straight code, and forms of
+// them taken in turn did not fit the instruction cache (products up to the cap and beyond it in one step, 25 % more passes:
+// 1 280 -> 3 885 us).
+template <bool BIAS>
+__device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, const RowBias& rb, const int4& vis, uint32_t s_addr, int ring, int page0, int kb0,
+                                            float& top) {
+  float2 sum = make_float2(0.f, 0.f);
+  top = 0.f;
+#pragma unroll 1
+  for (int q = 0; q < 2; ++q) {
+    float s[16];
+    ASPD_TMEM_LD16(s_addr + q * 16, s, 0);
+    const int nv = misc->nval[ring][page0 + q] & 255, kb = kb0 + q * 16;
+    const uint32_t mask = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb));
+    float2 dist = make_float2(0.f, 0.f);
+    if constexpr (BIAS) {
+      dist.x = (float)(misc->kpos[ring][page0 + q] - rb.pos);
+      dist.y = dist.x + 1.f;
+    }
+    tmem_wait_ld16(s);
+    float mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mx = fmaxf(mx, fmaxf(fabsf(s[i]), fabsf(s[i + 1])));
+    top = fmaxf(top, mx);
+    if (__any_sync(0xffffffffu, mx > c.sp.poly_limit)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = saturated(s[i], c.sp);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float2 z = __fmul2_rn(make_float2(s[i], s[i + 1]), make_float2(c.sp.cap_in, c.sp.cap_in)), u = __fmul2_rn(z, z);
+        float2 p = make_float2(c.sp.poly[5], c.sp.poly[5]);
+#pragma unroll
+        for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.poly[k], c.sp.poly[k]));
+        p = __fmul2_rn(p, z);
+        s[i] = p.x; s[i + 1] = p.y;
+      }
+    }
+    uint32_t p8[8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      float2 x = make_float2(s[i], s[i + 1]);
+      if constexpr (BIAS) {
+        x = __ffma2_rn(make_float2(rb.slope, rb.slope), dist, x);
+        dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
+      }
+      x.x = ex2((mask >> i) & 1u ? x.x : -INFINITY);
+      x.y = ex2((mask >> (i + 1)) & 1u ? x.y : -INFINITY);
+      sum = __fadd2_rn(sum, x);
+      p8[i >> 1] = pack_bf16(x.x, x.y);
+    }
+    ASPD_TMEM_ST8U(s_addr + q * 8, p8);
+  }
+  return sum.x + sum.y;
+}
+
+// Capped scores, with fixed references only (aspd_plan::fixed_ref): the exponentials are taken against 0 always, so that nothing but the
+// sums goes from key to key, and a row is two threads': eight warps to a group, thread (part, r) takes 32 of the 64 scores of
+// a half.  (Four warps a group, a thread to a row as in softmax_group_w2, were two softmax warps to a scheduler, which issued in half of
+// the cycles: @MEASURED@.)  A half is one pass with the short polynomial, which keeps the largest product; where that turns
+// out to be beyond the polynomial's range (scores above 0.6 of the cap) it is taken again by far_scores, and the warp's next half goes
+// there at once.  P lies over the thread's own scores: 16 columns at columns 0 and 32 of the half's 64.
+template <bool BIAS>
+__device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
+                                                     int item_end, int grp, int tpt) {
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, part = uniform((warp >> 2) & 1), r = tid & 127;
+  const int G = c.G;
+  volatile int* ab = &misc->abort_flag;
+  const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t s_base = tmem + lane_addr + COL_S + grp * 128 + part * 32, o_base = tmem + lane_addr + COL_O + grp * 128 + part * 64;
+  const uint32_t qbuf = base + W2_OFF_Q + grp * kTileBytes, obuf = base + W2_OFF_OUT + warp * 2048;
+  const uint32_t bar_sfull = bars + 8 * (WS_FULL + 2 * grp), bar_pfull = bars + 8 * (WP_FULL + 2 * grp),      // + 8 h
+                 bar_ofull = bars + 8 * (WO_FULL + grp), bar_qfull = bars + 8 * (WQ_FULL + grp);
+  auto next_item = [&](int idx) {
+    for (; idx < item_end; ++idx) {
+      const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
+      if (it.n_q_tok > grp * tpt) {
+        prep_tile_w2<256>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, tid & 255);
+        warp_arrive_w2(bar_qfull);
+        break;
+      }
+    }
+  };
+  next_item(item_begin);
+  int g = 0, sc[2] = {0, 0}, ic = 0;
+  bool dead = false;
+  for (int idx = item_begin; idx < item_end; ++idx) {
+    const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
+    const int n_tiles = (it.n_pages + 7) >> 3;
+    const int n_tok = min(tpt, it.n_q_tok - grp * tpt);
+    if (n_tok <= 0) { g += n_tiles; continue; }                // the block has no second tile
+    const int tl = token_of(c, r), M = n_tok * G, tok = it.q_tok0 + grp * tpt + tl;
+    int4 vis = make_int4(0, 0, 0, 0);                          // padding rows see nothing
+    RowBias rb = {0.f, 0};
+    if (r < M) vis = c.pd.tok_vis[tok];
+    if (BIAS && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
+    float l = 0.f;
+    bool far = false;                                           // the warp's last half had scores beyond the short polynomial
+    for (int t = 0; t < n_tiles; ++t, ++g) {
+      const int npg = min(8, it.n_pages - t * 8), halves = npg > 4 ? 2 : 1, ring = g & (kPageRingW2 - 1);
+      for (int h = 0; h < halves; ++h) {
+        dead |= !mbar_wait(bar_sfull + 8 * h, sc[h] & 1, ab);
+        ++sc[h];
+        tc_fence_after();
+        const int page0 = 4 * h + 2 * part, kb0 = it.key0 + t * kTile + page0 * 16;
+        // (the ring's entries stay for this group: see softmax_group_w2)
+        const int2 ye = *reinterpret_cast<const int2*>(&misc->nval[ring][page0]);
+        const bool plain = r >= M || (kb0 + 32 <= vis.x && (ye.x & 255) + (ye.y & 255) == 32);
+        const bool masked = __any_sync(0xffffffffu, !plain);
+        float sum, top;
+        uint32_t pk[16];
+        auto pass = [&](auto masked_tag) {
+          constexpr bool MASKED = decltype(masked_tag)::value;
+          float s[32];
+          ASPD_TMEM_LD32(s_base + h * 64, s, 0);
+          top = 0.f;
+          float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+          tmem_wait_ld32(s);
+#pragma unroll
+          for (int pg = 0; pg < 2; ++pg) {
+            const int nv = (pg ? ye.y : ye.x) & 255, kb = kb0 + pg * 16;
+            uint32_t mask = 0xFFFFu;
+            if constexpr (MASKED) mask = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb));
+            float2 dist = make_float2(0.f, 0.f);
+            if constexpr (BIAS) {
+              dist.x = (float)(misc->kpos[ring][page0 + pg] - rb.pos);
+              dist.y = dist.x + 1.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              float2 x = make_float2(s[pg * 16 + i], s[pg * 16 + i + 1]);
+              top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
+              const float2 u = __fmul2_rn(x, x);
+              float2 p = make_float2(c.sp.near[3], c.sp.near[3]);
+#pragma unroll
+              for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.near[k], c.sp.near[k]));
+              if constexpr (BIAS) {
+                x = __ffma2_rn(x, p, __fmul2_rn(make_float2(rb.slope, rb.slope), dist));
+                dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
+              } else {
+                x = __fmul2_rn(x, p);
+              }
+              if (MASKED && mask != 0xFFFFu) {
+                x.x = (mask >> i) & 1u ? x.x : -INFINITY;
+                x.y = (mask >> (i + 1)) & 1u ? x.y : -INFINITY;
+              }
+              x.x = ex2(x.x); x.y = ex2(x.y);
+              if (i & 2) sum1 = __fadd2_rn(sum1, x);
+              else sum0 = __fadd2_rn(sum0, x);
+              pk[pg * 8 + (i >> 1)] = pack_bf16(x.x, x.y);
+            }
+          }
+          sum0 = __fadd2_rn(sum0, sum1);
+          sum = sum0.x + sum0.y;
+        };
+        bool again = far;
+        if (!again) {
+          if (masked) pass(std::true_type());
+          else pass(std::false_type());
+          again = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
+        }
+        if (again) {
+          sum = far_scores<BIAS>(c, misc, rb, vis, s_base + h * 64, ring, page0, kb0, top);
+          far = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
+        } else {
+          ASPD_TMEM_ST16U(s_base + h * 64, pk);
+        }
+        l += sum;
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive_w2(bar_pfull + 8 * h);
+      }
+    }
+    // ---- the next query tile, beside the rest of this item; then the row's two sums meet, and each of its threads
+    // normalises and stores half of it, a warp's 32 rows by quarter rows through shared memory
+    next_item(idx + 1);
+    asm volatile("st.shared.f32 [%0], %1;" ::"r"(obuf + lane * 4), "f"(l) : "memory");
+    named_sync(1 + grp, 256);
+    {
+      float other;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(other) : "r"(obuf + (part ? -4 : 4) * 2048 + lane * 4) : "memory");
+      l += other;
+    }
+    named_sync(1 + grp, 256);                                   // before either buffer is written again
+    dead |= !mbar_wait(bar_ofull, ic & 1, ab);
+    tc_fence_after();
+    ++ic;
+    const float inv_l = l > 0.f ? 1.f / l : 0.f;
+    const int rw0 = (warp & 3) * 32, ch = lane & 3;
+    __nv_bfloat16* out0 = c.out + ((size_t)(it.q_tok0 + grp * tpt) * c.n_q_heads + it.kv_head * G) * 128 + part * 64 + ch * 8;
+#pragma unroll 1
+    for (int quarter = 0; quarter < 2; ++quarter) {
+      float o[32];
+      ASPD_TMEM_LD32(o_base + quarter * 32, o, 0);
+      tmem_wait_ld32(o);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(obuf + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)),
+                     "r"(pack_bf16(o[8 * i] * inv_l, o[8 * i + 1] * inv_l)), "r"(pack_bf16(o[8 * i + 2] * inv_l, o[8 * i + 3] * inv_l)),
+                     "r"(pack_bf16(o[8 * i + 4] * inv_l, o[8 * i + 5] * inv_l)), "r"(pack_bf16(o[8 * i + 6] * inv_l, o[8 * i + 7] * inv_l))
+                     : "memory");
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int rl = k * 8 + (lane >> 2), ro = rw0 + rl;
+        uint4 x;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                     : "r"(obuf + rl * 64 + ((ch ^ ((rl >> 1) & 3)) << 4)) : "memory");
+        if (ro < M && !dead) *reinterpret_cast<uint4*>(out0 + (size_t)(token_of(c, ro) * (c.n_q_heads - G) + ro) * 128 + quarter * 32) = x;
+      }
+      __syncwarp();
+    }
+    tc_fence_before();
+    if (named_sync_or(1 + grp, 256, dead || *ab)) break;
+  }
+}
+
 template <int SC>
-__global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
+__global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
+  // softmax warps 0 ..., then the K and V producers and the two groups' issuers
+  constexpr int kSoftmaxWarps = kSoftmaxWarpsW2<SC>, W2_KPROD = kSoftmaxWarps, W2_VPROD = kSoftmaxWarps + 1, W2_ISSUE = kSoftmaxWarps + 2;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -457,12 +644,13 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   if (page_positions && lane < head.w) first_pos = c.pd.page_pos[head.z + lane];
   {
     const int n_cached = min(item_end - item_begin, kItemCacheW2);
-    for (int e = tid; e < n_cached * (int)(sizeof(DeviceItem) / 4); e += kThreadsW2)
+    for (int e = tid; e < n_cached * (int)(sizeof(DeviceItem) / 4); e += kThreadsW2<SC>)
       reinterpret_cast<int*>(misc->items)[e] = reinterpret_cast<const int*>(c.pd.items + item_begin)[e];
   }
   if (tid == 0) {
+    constexpr int n = kSoftmaxWarps / 2;           // warps of a group
     //                               K_FULL K_EMPTY V_FULL V_EMPTY S_FULL(4)    P_FULL(4)   PV_DONE O_FULL Q_FULL
-    const int counts[W2_NUM_BARS] = {1, 1,  2, 2,   1, 1,  2, 2,   1, 1, 1, 1,  4, 4, 4, 4, 1, 1,   1, 1,  4, 4};
+    const int counts[W2_NUM_BARS] = {1, 1,  2, 2,   1, 1,  2, 2,   1, 1, 1, 1,  n, n, n, n, 1, 1,   1, 1,  n, n};
     for (int i = 0; i < W2_NUM_BARS; ++i) mbar_init(bars + 8 * i, counts[i]);
     misc->abort_flag = 0;
     misc->lead = item_begin;
@@ -485,8 +673,9 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
   if (!producer_runs_ahead) pdl_wait();
   if (tid == 0) ASPD_CTA_STAMP(c, 1);
 
-  if (warp < 8) {
-    softmax_group_w2<SC>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 2, tpt);
+  if (warp < kSoftmaxWarps) {
+    if constexpr (SC & kCapped) softmax_group_capped<(SC & kBiased) != 0>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 3, tpt);
+    else softmax_group_w2<(SC & kBiased) != 0>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 2, tpt);
   } else if (warp == W2_KPROD || warp == W2_VPROD) {
     // ================================ bulk-copy producers (as in the other variants) ================================
     const int kv = warp == W2_KPROD ? 0 : 1;
@@ -616,7 +805,7 @@ __global__ void __launch_bounds__(kThreadsW2, 1) attn_tc_w2_kernel(Ctx c) {
             tc_fence_after();
             if (lane == 0 && grp == 0) ASPD_STAMP(c, g, 10 + h);
             // 16 keys = one page per k-step
-            tc_mma_ts_pv_lane0(o_tmem, s_tmem + h * 64, smem_desc(vbuf + 4 * h * 4096, 1024, 2048), idesc_pv, (t > 0 || h > 0) ? 1u : 0u, min(4, npg - 4 * h));
+            tc_mma_ts_pv_lane0<SC & kCapped ? 32 : 16>(o_tmem, s_tmem + h * 64, smem_desc(vbuf + 4 * h * 4096, 1024, 2048), idesc_pv, (t > 0 || h > 0) ? 1u : 0u, min(4, npg - 4 * h));
             // (Asked for only when a row's reference moves.  Before the word of the scores behind it, which send the group
             // two halves on, and before O's: a group that waits for half hc - 1 then knows that half hc - 2 is through,
             // and the parity tells the two apart.)

@@ -103,8 +103,9 @@ __device__ __forceinline__ void tc_mma_ss_k128_lane0(uint32_t d_tmem, uint64_t a
       "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t}"
       ::"r"(d_tmem), "l"(a0), "l"(b0), "r"(idesc), "n"(A_HALF / 16), "n"(B_HALF / 16) : "memory");
 }
-// Up to four k-steps of 16 keys of O += P . V: P (bf16) in tensor memory, 8 columns per k-step; V
-// pages of 4096 bytes in shared memory.  `first_acc` = 0 overwrites the accumulator at the first k-step.
+// Up to four k-steps of 16 keys of O += P . V: P (bf16) in tensor memory, 8 columns per k-step, those of steps 2 and 3 from
+// column PAIR on; V pages of 4096 bytes in shared memory.  `first_acc` = 0 overwrites the accumulator at the first k-step.
+template <uint32_t PAIR>
 __device__ __forceinline__ void tc_mma_ts_pv_lane0(uint32_t d_tmem, uint32_t p_tmem, uint64_t v0, uint32_t idesc, uint32_t first_acc, int n) {
   asm volatile(
       "{\n\t.reg .pred e, f, o, q;\n\t.reg .u32 l;\n\t.reg .b32 t;\n\t.reg .b64 b;\n\t"
@@ -117,12 +118,12 @@ __device__ __forceinline__ void tc_mma_ts_pv_lane0(uint32_t d_tmem, uint32_t p_t
       "add.u32 t, %1, 8;\n\tadd.s64 b, %2, 256;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
       "setp.gt.and.s32 q, %5, 2, e;\n\t"
-      "add.u32 t, %1, 16;\n\tadd.s64 b, %2, 512;\n\t"
+      "add.u32 t, %1, %6;\n\tadd.s64 b, %2, 512;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
       "setp.gt.and.s32 q, %5, 3, e;\n\t"
-      "add.u32 t, %1, 24;\n\tadd.s64 b, %2, 768;\n\t"
+      "add.u32 t, %1, %6 + 8;\n\tadd.s64 b, %2, 768;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t}"
-      ::"r"(d_tmem), "r"(p_tmem), "l"(v0), "r"(idesc), "r"(first_acc), "r"(n) : "memory");
+      ::"r"(d_tmem), "r"(p_tmem), "l"(v0), "r"(idesc), "r"(first_acc), "r"(n), "n"(PAIR) : "memory");
 }
 // Up to eight k-steps of 16 keys of O += P . V with both operands in shared memory: P K-major in two
 // spans of 64 keys (A_HALF bytes apart), V pages of 4096 bytes.  `first_acc` = 0 overwrites the
@@ -206,6 +207,12 @@ __device__ __forceinline__ bool named_sync_or(int id, int n, bool pred) {
 #define ASPD_TMEM_ST8U(taddr, v)                                                                                  \
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"                    \
                ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(taddr) : "memory")
+// 16 uint32 of this thread -> 16 consecutive columns of its TMEM lane
+#define ASPD_TMEM_ST16U(taddr, v)                                                                                 \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "  \
+               "%12, %13, %14, %15};"                                                                             \
+               ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), \
+                 "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory")
 #define ASPD_TMEM_LD16(taddr, v, o)                                                                               \
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "  \
                "%13, %14, %15}, [%16];"                                                                          \
