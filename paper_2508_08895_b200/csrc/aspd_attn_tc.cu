@@ -114,6 +114,7 @@ struct Ctx {
   int G, inv_g;                // query heads of a KV head; 65536 / G rounded up (token_of)
   float scale_log2;            // (1 in the instances for plans with scores of their own)
   ScoreParams sp;              // those instances: what makes logits of the products
+  int split_q;                 // those instances: queries in two bf16 pieces (plans that rotate them)
   int early_fetch;             // plan promise: pages without new rows are not written by in-flight work
   int m64;                     // MMAs with M = 64: row blocks of at most 64 rows are not padded to 128 (half the tensor work)
   int pv64;                    // only P.V with M = 64 (scores and the softmax layout stay at M = 128): O then sits in 16 lanes
@@ -745,12 +746,20 @@ __device__ __forceinline__ bool softmax_item_wide(const Ctx& c, const DeviceItem
 // A operand.  Called by NT threads (rank 0 .. NT - 1); all loads of a thread's rows are issued
 // before the first use.  Unit e = (row e / 8, 16-byte chunk e % 8 of each span); a call covers
 // units e0 + rank + NT u, u < U (row blocks of 64 rows have 512 units, of 128 rows 1024).
-template <int U>
+// SPLIT: with what the rounding left over as a second tile (plans with scores of their own, where c.split_q): such scores are large -- a cap
+// is for those -- and a logit is off by what the rounding takes from a product.  Logits with a deviation of 5: outputs off from 64 bits by
+// 0.0045 (relative, root mean square) with queries rounded to bf16, 0.0024 in two pieces, 0.0017 of it by the output's own rounding.
+template <int U, bool SPLIT = false>
 struct QUnits {
   uint32_t lo[U][4], hi[U][4];   // per unit: the rotated chunk of the first and of the second span, bf16 pairs
+  uint32_t lo2[SPLIT ? U : 1][4], hi2[SPLIT ? U : 1][4];
 };
-template <int NT = 128, int U = 4>
-__device__ __forceinline__ void prep_q_compute(const Ctx& c, const DeviceItem& it, int rank, int e0, QUnits<U>& qu) {
+// a pair of bf16 and the pair of what is left
+__device__ __forceinline__ uint32_t pack_rest(float a, float b, uint32_t packed) {
+  return pack_bf16(a - __uint_as_float(packed << 16), b - __uint_as_float(packed & 0xffff0000u));
+}
+template <int NT = 128, int U = 4, bool SPLIT = false>
+__device__ __forceinline__ void prep_q_compute(const Ctx& c, const DeviceItem& it, int rank, int e0, QUnits<U, SPLIT>& qu) {
   const int G = c.G;
   const int M = it.n_q_tok * G, R = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
   uint4 a[U], b[U];
@@ -778,13 +787,19 @@ __device__ __forceinline__ void prep_q_compute(const Ctx& c, const DeviceItem& i
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 x0 = __bfloat1622float2(a2[i]), x1 = __bfloat1622float2(b2[i]);
-      qu.lo[u][i] = pack_bf16(x0.x * w[u][i].x - x1.x * w[u][i].y, x0.y * w[u][i].z - x1.y * w[u][i].w);
-      qu.hi[u][i] = pack_bf16(x1.x * w[u][i].x + x0.x * w[u][i].y, x1.y * w[u][i].z + x0.y * w[u][i].w);
+      const float2 y0 = make_float2(x0.x * w[u][i].x - x1.x * w[u][i].y, x0.y * w[u][i].z - x1.y * w[u][i].w);
+      const float2 y1 = make_float2(x1.x * w[u][i].x + x0.x * w[u][i].y, x1.y * w[u][i].z + x0.y * w[u][i].w);
+      qu.lo[u][i] = pack_bf16(y0.x, y0.y);
+      qu.hi[u][i] = pack_bf16(y1.x, y1.y);
+      if constexpr (SPLIT) {
+        qu.lo2[u][i] = pack_rest(y0.x, y0.y, qu.lo[u][i]);
+        qu.hi2[u][i] = pack_rest(y1.x, y1.y, qu.hi[u][i]);
+      }
     }
   }
 }
-template <int NT = 128, int U = 4>
-__device__ __forceinline__ void prep_q_store(const Ctx& c, const DeviceItem& it, uint32_t qbuf, int rank, int e0, const QUnits<U>& qu) {
+template <int NT = 128, int U = 4, bool SPLIT = false>
+__device__ __forceinline__ void prep_q_store(const Ctx& c, const DeviceItem& it, uint32_t qbuf, int rank, int e0, const QUnits<U, SPLIT>& qu) {
   const int G = c.G;
   const int M = it.n_q_tok * G, R = M <= 32 ? 32 : (M <= 64 ? 64 : 128), KS = (c.m64 ? 64 : 128) / R;
 #pragma unroll
@@ -797,14 +812,22 @@ __device__ __forceinline__ void prep_q_store(const Ctx& c, const DeviceItem& it,
                    "r"(qu.lo[u][3]) : "memory");
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kHalf), "r"(qu.hi[u][0]), "r"(qu.hi[u][1]), "r"(qu.hi[u][2]),
                    "r"(qu.hi[u][3]) : "memory");
+      if constexpr (SPLIT) {
+        if (c.split_q) {
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kTileBytes), "r"(qu.lo2[u][0]), "r"(qu.lo2[u][1]), "r"(qu.lo2[u][2]),
+                       "r"(qu.lo2[u][3]) : "memory");
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kTileBytes + kHalf), "r"(qu.hi2[u][0]), "r"(qu.hi2[u][1]), "r"(qu.hi2[u][2]),
+                       "r"(qu.hi2[u][3]) : "memory");
+        }
+      }
     }
   }
 }
-template <int NT = 128, int U = 4>
+template <int NT = 128, int U = 4, bool SPLIT = false>
 __device__ __forceinline__ void prep_q(const Ctx& c, const DeviceItem& it, uint32_t qbuf, int rank, int e0 = 0) {
-  QUnits<U> qu;
-  prep_q_compute<NT, U>(c, it, rank, e0, qu);
-  prep_q_store<NT, U>(c, it, qbuf, rank, e0, qu);
+  QUnits<U, SPLIT> qu;
+  prep_q_compute<NT, U, SPLIT>(c, it, rank, e0, qu);
+  prep_q_store<NT, U, SPLIT>(c, it, qbuf, rank, e0, qu);
 }
 
 // Fused step (aspd_branch_step / aspd_serial_step): the rows this step adds to pages that THIS CTA
@@ -910,6 +933,8 @@ enum { kPlain = 0, kOptions = 1, kPatch = 2 };
 template <bool WIDE, int MODE, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
   constexpr bool OPT = MODE == kOptions, PATCH = MODE == kPatch, SC = SCORES != kProducts;
+  // the second piece of the queries lies where the next item's tile would be; then, as in the wide variant, there is one query tile
+  constexpr bool SPLIT = SC && !WIDE, ONE_Q = WIDE || SPLIT;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -984,7 +1009,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
     // =============================== softmax ===============================
     // The first query tile, while the first K/V tiles are in flight and the epilogue threads write the new rows.
     if (item_begin < item_end) {
-      prep_q<kSoftmaxThreads, WIDE ? 4 : 2>(c, get_item(c, misc, item_begin, item_begin), base + OFF_Q, tid);
+      prep_q<kSoftmaxThreads, WIDE ? 4 : 2, SPLIT>(c, get_item(c, misc, item_begin, item_begin), base + OFF_Q, tid);
       fence_async_smem();
       mbar_arrive(bars + 8 * Q_FULL);
       named_sync(1, kSoftmaxThreads);              // the items' ranges are there
@@ -1104,9 +1129,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const uint32_t full_mask = 0xffffffffu;
       const uint32_t tmem_u = __shfl_sync(full_mask, tmem, 0);
       const uint32_t base_u = __shfl_sync(full_mask, base, 0), bars_u = base_u + off_misc;
-      struct TileRef { int npg, first, last, qb, ob, item_no, fresh; };   // qb: query tile (always 0 in the wide kernel); fresh:
+      struct TileRef { int npg, first, last, qb, ob, item_no, fresh; };   // qb: query tile (always 0 where there is one); fresh:
                                                                           // 1 + number among the slot's tiles with new rows (0: none)
-      auto q_fill = [](int item_no) { return WIDE ? item_no : item_no >> 1; };   // how often the item's query tile was filled before
+      auto q_fill = [](int item_no) { return ONE_Q ? item_no : item_no >> 1; };   // how often the item's query tile was filled before
       auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(full_mask, mbar_wait(bar, parity, ab)) != 0; };
       const uint32_t mma_m = OPT && c.m64 ? 64u : 128u;
       const uint32_t idesc_pv = instr_desc(128, 1, ((OPT && c.m64) || c.pv64) ? 64u : 128u);
@@ -1129,6 +1154,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
         const uint32_t idesc_s = instr_desc((uint32_t)tr.npg * 16u, 0, mma_m);
         // k-step ks covers head_dim elements [16 ks, 16 ks + 16): span ks / 4, 32 bytes per step
         tc_mma_ss_k128_lane0<kHalf, 1024>(tmem_u + COL_S + sb * 128, smem_desc(qbuf, 16, 1024), smem_desc(kbuf, 16, 2048), idesc_s);
+        if constexpr (SPLIT) {
+          if (c.split_q)
+            tc_mma_ss_k128_lane0<kHalf, 1024, true>(tmem_u + COL_S + sb * 128, smem_desc(qbuf + kTileBytes, 16, 1024), smem_desc(kbuf, 16, 2048), idesc_s);
+        }
         if (lane == 0) ASPD_STAMP(c, g, 9);
         tc_commit_lane0(bars_u + 8 * (S_FULL + sb));
         tc_commit_lane0(bars_u + 8 * (K_EMPTY + sb));
@@ -1160,7 +1189,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       for (int idx = ib; idx < ie && ok; ++idx, ++item_no) {
         const int n_pages = get_item(c, misc, idx, ib).n_pages, n_tiles = (n_pages + 7) >> 3;
         for (int t = 0; t < n_tiles && ok; ++t, ++g) {
-          TileRef cur = {min(8, n_pages - t * 8), t == 0, t == n_tiles - 1, WIDE ? 0 : item_no & 1, item_no & 1, item_no, 0};
+          TileRef cur = {min(8, n_pages - t * 8), t == 0, t == n_tiles - 1, ONE_Q ? 0 : item_no & 1, item_no & 1, item_no, 0};
           ok = issue_s(cur, g);
           if (ok && have_prev) ok = issue_pv(prev, g - 1);
           prev = cur;
@@ -1193,8 +1222,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const int ob = item_no & 1, M = it.n_q_tok * G, R = M <= 32 ? 32 : (M <= 64 ? 64 : 128),
                 KS = ((OPT && c.m64) ? 64 : 128) / R;                // replicas in the softmax threads' layout
       if (idx + 1 < item_end) {                    // the next item's query tile: into the other buffer, or (wide
-        const int qn = WIDE ? 0 : (item_no + 1) & 1;   // kernel) into the only one once this item's last S is issued
-        const int fills = WIDE ? item_no + 1 : (item_no + 1) >> 1;
+        const int qn = ONE_Q ? 0 : (item_no + 1) & 1;   // kernel) into the only one once this item's last S is issued
+        const int fills = ONE_Q ? item_no + 1 : (item_no + 1) >> 1;
         if constexpr (WIDE) {
           // the only query tile is free once this item's last S has been issued: rotate the next
           // item's rows into registers first, so that only the stores are left for after the wait
@@ -1205,6 +1234,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
           dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
           prep_q_store(c, nx, base + OFF_Q, et, 0, q0);
           prep_q_store(c, nx, base + OFF_Q, et, 512, q1);
+        } else if constexpr (SPLIT) {
+          const DeviceItem nx = get_item(c, misc, idx + 1, item_begin);
+          QUnits<4, true> q0;
+          prep_q_compute<128, 4, true>(c, nx, et, 0, q0);
+          dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
+          prep_q_store<128, 4, true>(c, nx, base + OFF_Q, et, 0, q0);
         } else {
           dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
           prep_q(c, get_item(c, misc, idx + 1, item_begin), base + OFF_Q + qn * kTileBytes, et);
@@ -1432,6 +1467,7 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
   c.inv_g = (65536 + c.G - 1) / c.G;
   c.scale_log2 = p->scored() ? 1.f : sh.sm_scale * kLog2e;
   c.sp = score_params(p);
+  c.split_q = p->rotated ? 0 : 1;
   c.early_fetch = p->stable_cache;
   c.stagger_start = p->stagger_start;
   c.m64 = (p->m64 == 1 && !p->wide && !p->dealt) ? 1 : 0;

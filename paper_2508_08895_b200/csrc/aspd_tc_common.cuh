@@ -77,14 +77,14 @@ __device__ __forceinline__ void tc_commit_lane0(uint32_t bar) {
 //
 // Eight k-steps of a 128 x N x 128 product with both operands in shared memory (K-major, 128-byte
 // swizzle): k-step ks reads A at +32 (ks % 4) bytes in half ks / 4 (a_half bytes apart), B likewise
-// with halves b_half bytes apart.  Lane 0 issues; the first k-step overwrites the accumulator.
-template <uint32_t A_HALF, uint32_t B_HALF>
+// with halves b_half bytes apart.  Lane 0 issues; the first k-step overwrites the accumulator, or (ACC) adds to it.
+template <uint32_t A_HALF, uint32_t B_HALF, bool ACC = false>
 __device__ __forceinline__ void tc_mma_ss_k128_lane0(uint32_t d_tmem, uint64_t a0, uint64_t b0, uint32_t idesc) {
   asm volatile(
       "{\n\t.reg .pred e, z, o;\n\t.reg .u32 l;\n\t.reg .b64 a, b;\n\t"
       "mov.u32 l, %%laneid;\n\t"
       "setp.eq.u32 e, l, 0;\n\t"
-      "setp.ne.b32 z, 0, 0;\n\t"
+      "setp.ne.b32 z, %6, 0;\n\t"
       "setp.eq.b32 o, 0, 0;\n\t"
       "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, z;\n\t"
       "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
@@ -101,7 +101,7 @@ __device__ __forceinline__ void tc_mma_ss_k128_lane0(uint32_t d_tmem, uint64_t a
       "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
       "add.s64 a, %1, %4 + 6;\n\tadd.s64 b, %2, %5 + 6;\n\t"
       "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t}"
-      ::"r"(d_tmem), "l"(a0), "l"(b0), "r"(idesc), "n"(A_HALF / 16), "n"(B_HALF / 16) : "memory");
+      ::"r"(d_tmem), "l"(a0), "l"(b0), "r"(idesc), "n"(A_HALF / 16), "n"(B_HALF / 16), "n"(ACC ? 1 : 0) : "memory");
 }
 // Up to four k-steps of 16 keys of O += P . V: P (bf16) in tensor memory, 8 columns per k-step, those of steps 2 and 3 from
 // column PAIR on; V pages of 4096 bytes in shared memory.  `first_acc` = 0 overwrites the accumulator at the first k-step.
