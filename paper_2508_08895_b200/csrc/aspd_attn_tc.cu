@@ -934,7 +934,8 @@ template <bool WIDE, int MODE, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
   constexpr bool OPT = MODE == kOptions, PATCH = MODE == kPatch, SC = SCORES != kProducts;
   // the second piece of the queries lies where the next item's tile would be; then, as in the wide variant, there is one query tile
-  constexpr bool SPLIT = SC && !WIDE, ONE_Q = WIDE || SPLIT;
+  constexpr bool SPLIT = SC && !WIDE;
+  const bool one_q = WIDE || (SPLIT && c.split_q);
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -1131,7 +1132,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const uint32_t base_u = __shfl_sync(full_mask, base, 0), bars_u = base_u + off_misc;
       struct TileRef { int npg, first, last, qb, ob, item_no, fresh; };   // qb: query tile (always 0 where there is one); fresh:
                                                                           // 1 + number among the slot's tiles with new rows (0: none)
-      auto q_fill = [](int item_no) { return ONE_Q ? item_no : item_no >> 1; };   // how often the item's query tile was filled before
+      auto q_fill = [one_q](int item_no) { return one_q ? item_no : item_no >> 1; };   // how often the item's query tile was filled before
       auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(full_mask, mbar_wait(bar, parity, ab)) != 0; };
       const uint32_t mma_m = OPT && c.m64 ? 64u : 128u;
       const uint32_t idesc_pv = instr_desc(128, 1, ((OPT && c.m64) || c.pv64) ? 64u : 128u);
@@ -1189,7 +1190,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       for (int idx = ib; idx < ie && ok; ++idx, ++item_no) {
         const int n_pages = get_item(c, misc, idx, ib).n_pages, n_tiles = (n_pages + 7) >> 3;
         for (int t = 0; t < n_tiles && ok; ++t, ++g) {
-          TileRef cur = {min(8, n_pages - t * 8), t == 0, t == n_tiles - 1, ONE_Q ? 0 : item_no & 1, item_no & 1, item_no, 0};
+          TileRef cur = {min(8, n_pages - t * 8), t == 0, t == n_tiles - 1, one_q ? 0 : item_no & 1, item_no & 1, item_no, 0};
           ok = issue_s(cur, g);
           if (ok && have_prev) ok = issue_pv(prev, g - 1);
           prev = cur;
@@ -1222,8 +1223,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const int ob = item_no & 1, M = it.n_q_tok * G, R = M <= 32 ? 32 : (M <= 64 ? 64 : 128),
                 KS = ((OPT && c.m64) ? 64 : 128) / R;                // replicas in the softmax threads' layout
       if (idx + 1 < item_end) {                    // the next item's query tile: into the other buffer, or (wide
-        const int qn = ONE_Q ? 0 : (item_no + 1) & 1;   // kernel) into the only one once this item's last S is issued
-        const int fills = ONE_Q ? item_no + 1 : (item_no + 1) >> 1;
+        const int qn = one_q ? 0 : (item_no + 1) & 1;   // kernel) into the only one once this item's last S is issued
+        const int fills = one_q ? item_no + 1 : (item_no + 1) >> 1;
         if constexpr (WIDE) {
           // the only query tile is free once this item's last S has been issued: rotate the next
           // item's rows into registers first, so that only the stores are left for after the wait
@@ -1239,7 +1240,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
           QUnits<4, true> q0;
           prep_q_compute<128, 4, true>(c, nx, et, 0, q0);
           dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
-          prep_q_store<128, 4, true>(c, nx, base + OFF_Q, et, 0, q0);
+          prep_q_store<128, 4, true>(c, nx, base + OFF_Q + qn * kTileBytes, et, 0, q0);
         } else {
           dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
           prep_q(c, get_item(c, misc, idx + 1, item_begin), base + OFF_Q + qn * kTileBytes, et);

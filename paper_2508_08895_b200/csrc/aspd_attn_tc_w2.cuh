@@ -40,7 +40,12 @@ template <int SCORES> constexpr int kThreadsW2 = (kSoftmaxWarpsW2<SCORES> + 4) *
 constexpr uint32_t W2_OFF_K = 0, W2_OFF_V = 2 * kTileBytes, W2_OFF_Q = 4 * kTileBytes, W2_OFF_OUT = 6 * kTileBytes,
                    W2_OFF_MISC = 7 * kTileBytes;
 constexpr size_t kSmemBytesW2 = 7 * kTileBytes + 2048 + 1024;   // + Misc + slack to align the base to 1024
-constexpr int kItemCacheW2 = 8;
+constexpr int kItemCacheW2 = 7;
+// Capped scores (softmax_group_capped): a stage of K or V is 64 keys, three of either, and a group has two query tiles, the second with what
+// the rounding of the first left over (QUnits).
+constexpr int kStagesW2c = 3;
+constexpr uint32_t kStageW2c = 16384, W2C_OFF_K = 0, W2C_OFF_V = kStagesW2c * kStageW2c, W2C_OFF_Q = 2 * kStagesW2c * kStageW2c;
+static_assert(W2C_OFF_Q + 4 * kTileBytes <= W2_OFF_MISC, "the query tiles must fit before Misc");
 constexpr int kPageRingW2 = 8;      // tiles whose page entries are kept: a group may be read up to four tiles late (see softmax_group_w2)
 // The reference maximum of a row is raised when an exponent passes 2^40 (everything is floating point,
 // bf16 and fp32 alike, so the distance costs no precision; what must not happen is an overflow, and
@@ -48,8 +53,8 @@ constexpr int kPageRingW2 = 8;      // tiles whose page entries are kept: a grou
 constexpr float kRaiseW2 = 40.0f, kRaiseSumW2 = 1099511627776.0f;
 
 // S_FULL / P_FULL: one per (group, half of the tile's keys)
-enum BarW2 { WK_FULL = 0, WK_EMPTY = 2, WV_FULL = 4, WV_EMPTY = 6, WS_FULL = 8, WP_FULL = 12, WPV_DONE = 16, WO_FULL = 18, WQ_FULL = 20,
-             W2_NUM_BARS = 22 };
+enum BarW2 { WK_FULL = 0, WK_EMPTY = 3, WV_FULL = 6, WV_EMPTY = 9, WS_FULL = 12, WP_FULL = 16, WPV_DONE = 20, WO_FULL = 22, WQ_FULL = 24,
+             W2_NUM_BARS = 26 };
 
 struct MiscW2 {
   uint64_t bars[W2_NUM_BARS];
@@ -59,6 +64,7 @@ struct MiscW2 {
   int abort_flag;
   int lead;                          // the item group 0's issuer is at (read by group 1's)
   int kpos[kPageRingW2][8];          // plans with a distance bias: position IDs of the pages' first rows (ring as nval)
+  float lsum[2][128];                // capped scores, per group: where a row's two sums meet
 };
 static_assert(sizeof(MiscW2) <= 2048, "MiscW2 must fit behind the tiles");
 
@@ -76,7 +82,8 @@ __device__ __forceinline__ void warp_arrive_w2(uint32_t bar) {
 // The group's query tile of an item: rows rotated (RoPE at the token's position, cos/sin table of the plan), bf16,
 // as the 128-byte-swizzled K-major A operand (rows beyond the item's are zero).  A thread takes the 16-byte chunk
 // `rank % 8` of both halves of rows rank / 8 + NT / 8 u; all of its query loads are on their way before the first is used.
-template <int NT>
+// SPLIT: what the rounding leaves over goes to a second tile, two tiles on (where c.split_q).
+template <int NT, bool SPLIT>
 __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok, int kv_head, uint32_t qbuf, int rank) {
   const int G = c.G, M = n_tok * G, ch = rank & 7, row0 = rank >> 3;
   const __nv_bfloat16* q0 = c.q + ((size_t)q_tok0 * c.n_q_heads + kv_head * G) * 128 + ch * 8;
@@ -99,17 +106,25 @@ __device__ __forceinline__ void prep_tile_w2(const Ctx& c, int q_tok0, int n_tok
     const float4* cs = cs0 + (size_t)(r < M ? tl : 0) * 32;
     const __nv_bfloat162* a2 = reinterpret_cast<const __nv_bfloat162*>(&a[u]);
     const __nv_bfloat162* b2 = reinterpret_cast<const __nv_bfloat162*>(&b[u]);
-    uint32_t lo[4], hi[4];
+    uint32_t lo[4], hi[4], lo2[4], hi2[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float4 w = cs[i];
       const float2 x0 = __bfloat1622float2(a2[i]), x1 = __bfloat1622float2(b2[i]);
-      lo[i] = pack_bf16(x0.x * w.x - x1.x * w.y, x0.y * w.z - x1.y * w.w);
-      hi[i] = pack_bf16(x1.x * w.x + x0.x * w.y, x1.y * w.z + x0.y * w.w);
+      const float2 y0 = make_float2(x0.x * w.x - x1.x * w.y, x0.y * w.z - x1.y * w.w), y1 = make_float2(x1.x * w.x + x0.x * w.y, x1.y * w.z + x0.y * w.w);
+      lo[i] = pack_bf16(y0.x, y0.y);
+      hi[i] = pack_bf16(y1.x, y1.y);
+      if constexpr (SPLIT) { lo2[i] = pack_rest(y0.x, y0.y, lo[i]); hi2[i] = pack_rest(y1.x, y1.y, hi[i]); }
     }
     const uint32_t addr = qbuf + r * 128 + ((ch ^ (r & 7)) << 4);
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kHalf), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+    if constexpr (SPLIT) {
+      if (c.split_q) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + 2 * kTileBytes), "r"(lo2[0]), "r"(lo2[1]), "r"(lo2[2]), "r"(lo2[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + 2 * kTileBytes + kHalf), "r"(hi2[0]), "r"(hi2[1]), "r"(hi2[2]), "r"(hi2[3]) : "memory");
+      }
+    }
   }
   fence_async_smem();
 }
@@ -131,7 +146,7 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
     for (; idx < item_end; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
       if (it.n_q_tok > grp * tpt) {
-        prep_tile_w2<128>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, r);
+        prep_tile_w2<128, false>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, r);
         warp_arrive_w2(bar_qfull);
         break;
       }
@@ -408,19 +423,19 @@ __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, co
 template <bool BIAS>
 __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                      int item_end, int grp, int tpt) {
-  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, part = uniform((warp >> 2) & 1), r = tid & 127;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), part = uniform((warp >> 2) & 1), r = tid & 127;
   const int G = c.G;
   volatile int* ab = &misc->abort_flag;
   const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
   const uint32_t s_base = tmem + lane_addr + COL_S + grp * 128 + part * 32, o_base = tmem + lane_addr + COL_O + grp * 128 + part * 64;
-  const uint32_t qbuf = base + W2_OFF_Q + grp * kTileBytes, obuf = base + W2_OFF_OUT + warp * 2048;
+  const uint32_t qbuf = base + W2C_OFF_Q + grp * kTileBytes;
   const uint32_t bar_sfull = bars + 8 * (WS_FULL + 2 * grp), bar_pfull = bars + 8 * (WP_FULL + 2 * grp),      // + 8 h
                  bar_ofull = bars + 8 * (WO_FULL + grp), bar_qfull = bars + 8 * (WQ_FULL + grp);
   auto next_item = [&](int idx) {
     for (; idx < item_end; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
       if (it.n_q_tok > grp * tpt) {
-        prep_tile_w2<256>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, tid & 255);
+        prep_tile_w2<256, true>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, tid & 255);
         warp_arrive_w2(bar_qfull);
         break;
       }
@@ -431,9 +446,9 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
   bool dead = false;
   for (int idx = item_begin; idx < item_end; ++idx) {
     const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
-    const int n_tiles = (it.n_pages + 7) >> 3;
+    const int n_halves = (it.n_pages + 3) >> 2;
     const int n_tok = min(tpt, it.n_q_tok - grp * tpt);
-    if (n_tok <= 0) { g += n_tiles; continue; }                // the block has no second tile
+    if (n_tok <= 0) { g += n_halves; continue; }               // the block has no second tile
     const int tl = token_of(c, r), M = n_tok * G, tok = it.q_tok0 + grp * tpt + tl;
     int4 vis = make_int4(0, 0, 0, 0);                          // padding rows see nothing
     RowBias rb = {0.f, 0};
@@ -441,14 +456,14 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
     if (BIAS && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
     float l = 0.f;
     bool far = false;                                           // the warp's last half had scores beyond the short polynomial
-    for (int t = 0; t < n_tiles; ++t, ++g) {
-      const int npg = min(8, it.n_pages - t * 8), halves = npg > 4 ? 2 : 1, ring = g & (kPageRingW2 - 1);
-      for (int h = 0; h < halves; ++h) {
+    for (int t = 0; t < n_halves; ++t, ++g) {
+      const int h = t & 1, ring = g & (kPageRingW2 - 1);         // h: which of the group's two score buffers
+      {
         dead |= !mbar_wait(bar_sfull + 8 * h, sc[h] & 1, ab);
         ++sc[h];
         tc_fence_after();
-        const int page0 = 4 * h + 2 * part, kb0 = it.key0 + t * kTile + page0 * 16;
-        // (the ring's entries stay for this group: see softmax_group_w2)
+        const int page0 = 2 * part, kb0 = it.key0 + t * 64 + page0 * 16;
+        // (The entries stay for this group: K of half g + 5 waits for scores of half g + 2, those for the group's P.V of half g.)
         const int2 ye = *reinterpret_cast<const int2*>(&misc->nval[ring][page0]);
         const bool plain = r >= M || (kb0 + 32 <= vis.x && (ye.x & 255) + (ye.y & 255) == 32);
         const bool masked = __any_sync(0xffffffffu, !plain);
@@ -517,43 +532,30 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
       }
     }
     // ---- the next query tile, beside the rest of this item; then the row's two sums meet, and each of its threads
-    // normalises and stores half of it, a warp's 32 rows by quarter rows through shared memory
+    // normalises and stores half of it (there is no room left to bring eight lanes' 16 bytes together; the stores are 4 % of
+    // a long item's lines)
     next_item(idx + 1);
-    asm volatile("st.shared.f32 [%0], %1;" ::"r"(obuf + lane * 4), "f"(l) : "memory");
+    if (part == 1) misc->lsum[grp][r] = l;
     named_sync(1 + grp, 256);
-    {
-      float other;
-      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(other) : "r"(obuf + (part ? -4 : 4) * 2048 + lane * 4) : "memory");
-      l += other;
-    }
-    named_sync(1 + grp, 256);                                   // before either buffer is written again
+    if (part == 0) misc->lsum[grp][r] += l;
+    named_sync(1 + grp, 256);
+    l = misc->lsum[grp][r];
     dead |= !mbar_wait(bar_ofull, ic & 1, ab);
     tc_fence_after();
     ++ic;
     const float inv_l = l > 0.f ? 1.f / l : 0.f;
-    const int rw0 = (warp & 3) * 32, ch = lane & 3;
-    __nv_bfloat16* out0 = c.out + ((size_t)(it.q_tok0 + grp * tpt) * c.n_q_heads + it.kv_head * G) * 128 + part * 64 + ch * 8;
+    uint4* dst = reinterpret_cast<uint4*>(c.out + ((size_t)tok * c.n_q_heads + it.kv_head * G + r - tl * G) * 128 + part * 64);
 #pragma unroll 1
     for (int quarter = 0; quarter < 2; ++quarter) {
       float o[32];
       ASPD_TMEM_LD32(o_base + quarter * 32, o, 0);
       tmem_wait_ld32(o);
+      if (r < M && !dead) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(obuf + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)),
-                     "r"(pack_bf16(o[8 * i] * inv_l, o[8 * i + 1] * inv_l)), "r"(pack_bf16(o[8 * i + 2] * inv_l, o[8 * i + 3] * inv_l)),
-                     "r"(pack_bf16(o[8 * i + 4] * inv_l, o[8 * i + 5] * inv_l)), "r"(pack_bf16(o[8 * i + 6] * inv_l, o[8 * i + 7] * inv_l))
-                     : "memory");
-      __syncwarp();
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int rl = k * 8 + (lane >> 2), ro = rw0 + rl;
-        uint4 x;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
-                     : "r"(obuf + rl * 64 + ((ch ^ ((rl >> 1) & 3)) << 4)) : "memory");
-        if (ro < M && !dead) *reinterpret_cast<uint4*>(out0 + (size_t)(token_of(c, ro) * (c.n_q_heads - G) + ro) * 128 + quarter * 32) = x;
+        for (int i = 0; i < 4; ++i)
+          dst[quarter * 4 + i] = make_uint4(pack_bf16(o[8 * i] * inv_l, o[8 * i + 1] * inv_l), pack_bf16(o[8 * i + 2] * inv_l, o[8 * i + 3] * inv_l),
+                                            pack_bf16(o[8 * i + 4] * inv_l, o[8 * i + 5] * inv_l), pack_bf16(o[8 * i + 6] * inv_l, o[8 * i + 7] * inv_l));
       }
-      __syncwarp();
     }
     tc_fence_before();
     if (named_sync_or(1 + grp, 256, dead || *ab)) break;
@@ -563,6 +565,7 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
 template <int SC>
 __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
   // softmax warps 0 ..., then the K and V producers and the two groups' issuers
+  constexpr bool CAPPED = (SC & kCapped) != 0;
   constexpr int kSoftmaxWarps = kSoftmaxWarpsW2<SC>, W2_KPROD = kSoftmaxWarps, W2_VPROD = kSoftmaxWarps + 1, W2_ISSUE = kSoftmaxWarps + 2;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -588,8 +591,8 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
   }
   if (tid == 0) {
     constexpr int n = kSoftmaxWarps / 2;           // warps of a group
-    //                               K_FULL K_EMPTY V_FULL V_EMPTY S_FULL(4)    P_FULL(4)   PV_DONE O_FULL Q_FULL
-    const int counts[W2_NUM_BARS] = {1, 1,  2, 2,   1, 1,  2, 2,   1, 1, 1, 1,  n, n, n, n, 1, 1,   1, 1,  n, n};
+    //                               K_FULL   K_EMPTY  V_FULL   V_EMPTY  S_FULL(4)   P_FULL(4)   PV_DONE O_FULL Q_FULL
+    const int counts[W2_NUM_BARS] = {1, 1, 1, 2, 2, 2, 1, 1, 1, 2, 2, 2, 1, 1, 1, 1, n, n, n, n, 1, 1,   1, 1,  n, n};
     for (int i = 0; i < W2_NUM_BARS; ++i) mbar_init(bars + 8 * i, counts[i]);
     misc->abort_flag = 0;
     misc->lead = item_begin;
@@ -613,28 +616,32 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
   if (tid == 0) ASPD_CTA_STAMP(c, 1);
 
   if (warp < kSoftmaxWarps) {
-    if constexpr (SC & kCapped) softmax_group_capped<(SC & kBiased) != 0>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 3, tpt);
+    if constexpr (CAPPED) softmax_group_capped<(SC & kBiased) != 0>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 3, tpt);
     else softmax_group_w2<(SC & kBiased) != 0>(c, misc, bars, base, tmem, item_begin, item_end, warp >> 2, tpt);
   } else if (warp == W2_KPROD || warp == W2_VPROD) {
     // ================================ bulk-copy producers (as in the other variants) ================================
+    // a stage: a tile of eight pages, two of them; capped: four pages, three of them
+    constexpr int kPages = CAPPED ? 4 : 8, kStages = CAPPED ? kStagesW2c : 2, kBatch = 32 / kPages;
+    constexpr uint32_t kBytes = kPages * 4096u;
     const int kv = warp == W2_KPROD ? 0 : 1;
     const char* pool = kv ? c.v_pool : c.k_pool;
-    int g = 0;
+    const uint32_t dst0 = base + (CAPPED ? (kv ? W2C_OFF_V : W2C_OFF_K) : (kv ? W2_OFF_V : W2_OFF_K));
+    int g = 0, sl = 0, fill = 0;                     // stages so far; place of the next one in its ring, and how often that was filled
     bool ok = true, waited = false;
     int2 nxt = first_pages;
     int nxt_pos = first_pos;
     for (int idx = item_begin; idx < item_end && ok; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
-      const int n_tiles = (it.n_pages + 7) >> 3;
+      const int n_stages = (it.n_pages + kPages - 1) / kPages;
       int2 cur = make_int2(0, 0);
       int cur_pos = 0;
-      for (int t = 0; t < n_tiles && ok; ++t, ++g) {
-        if ((t & 3) == 0) {
+      for (int t = 0; t < n_stages && ok; ++t, ++g) {
+        if (t % kBatch == 0) {
           cur = nxt;
           nxt = make_int2(0, 0);
           if constexpr (SC & kBiased) { cur_pos = nxt_pos; nxt_pos = 0; }
-          const int ahead = (t + 4) * 8 + lane;
-          if ((t + 4) * 8 < it.n_pages) {
+          const int first = (t + kBatch) * kPages, ahead = first + lane;
+          if (first < it.n_pages) {
             if (ahead < it.n_pages) nxt = c.pd.visit[it.page0 + ahead];
             if (page_positions && ahead < it.n_pages) nxt_pos = c.pd.page_pos[it.page0 + ahead];
           } else if (idx + 1 < item_end) {          // first batch of the next item
@@ -643,10 +650,10 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
             if (page_positions && lane < nx.n_pages) nxt_pos = c.pd.page_pos[nx.page0 + lane];
           }
         }
-        const int npg = min(8, it.n_pages - t * 8), sl = g & 1;
+        const int npg = min(kPages, it.n_pages - t * kPages), from = (t % kBatch) * kPages + (lane & (kPages - 1));
         int2 pg;
-        pg.x = __shfl_sync(0xffffffffu, cur.x, (t & 3) * 8 + (lane & 7));
-        pg.y = __shfl_sync(0xffffffffu, cur.y, (t & 3) * 8 + (lane & 7));
+        pg.x = __shfl_sync(0xffffffffu, cur.x, from);
+        pg.y = __shfl_sync(0xffffffffu, cur.y, from);
         if (lane >= npg) pg = make_int2(0, 0);
         if (lane < npg && !bounds_ok(c.pd, pg.x, 0, 16)) pg.x = 0;
         if (producer_runs_ahead && !waited && __any_sync(0xffffffffu, ((pg.y >> 8) & 31) != 0)) {
@@ -655,23 +662,91 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
         }
         const uint32_t full = bars + 8 * ((kv ? WV_FULL : WK_FULL) + sl), empty = bars + 8 * ((kv ? WV_EMPTY : WK_EMPTY) + sl);
         int good = 1;
-        if (lane == 0) good = mbar_wait(empty, ((g >> 1) & 1) ^ 1, ab) ? 1 : 0;
+        if (lane == 0) good = mbar_wait(empty, (fill & 1) ^ 1, ab) ? 1 : 0;
         good = __shfl_sync(0xffffffffu, good, 0);
         if (!good) { ok = false; break; }
         if (lane == 0) ASPD_STAMP(c, g, 13 + kv);
-        if (kv == 0 && lane < 8) misc->nval[g & (kPageRingW2 - 1)][lane] = pg.y;   // read by the softmax groups of tile g
+        if (kv == 0 && lane < kPages) misc->nval[g & (kPageRingW2 - 1)][lane] = pg.y;   // read by the softmax groups
         if constexpr (SC & kBiased) {
-          const int kp = __shfl_sync(0xffffffffu, cur_pos, (t & 3) * 8 + (lane & 7));
-          if (page_positions && lane < 8) misc->kpos[g & (kPageRingW2 - 1)][lane] = kp;
+          const int kp = __shfl_sync(0xffffffffu, cur_pos, from);
+          if (page_positions && lane < kPages) misc->kpos[g & (kPageRingW2 - 1)][lane] = kp;
         }
         __syncwarp();
         if (lane == 0) mbar_expect_tx(full, (uint32_t)npg * 4096u);
         __syncwarp();
-        if (lane < npg)
-          bulk_copy(base + (kv ? W2_OFF_V : W2_OFF_K) + sl * kTileBytes + lane * 4096,
-                    pool + ((size_t)pg.x * c.n_kv_heads + it.kv_head) * 4096, 4096, full);
+        if (lane < npg) bulk_copy(dst0 + sl * kBytes + lane * 4096, pool + ((size_t)pg.x * c.n_kv_heads + it.kv_head) * 4096, 4096, full);
+        if (++sl == kStages) { sl = 0; ++fill; }
       }
     }
+  } else if constexpr (CAPPED) {
+    // ============================ MMA issuers, capped scores (warp 18: group 0, warp 19: group 1) ============================
+    // As below, by halves of 64 keys with a stage each: P.V of half v as soon as its P is there, scores of half v + 2 right behind, which
+    // go over it.  Scores are two products where the queries come in two pieces.
+    const int grp = warp - W2_ISSUE;
+    const uint32_t fm = 0xffffffffu;
+    const uint32_t tmem_u = __shfl_sync(fm, tmem, 0), base_u = __shfl_sync(fm, base, 0), bars_u = base_u + W2_OFF_MISC;
+    const int ib = item_begin, ie = item_end;
+    auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(fm, mbar_wait(bar, parity, ab)) != 0; };
+    volatile int* lead = &misc->lead;                  // (see below)
+    const uint32_t idesc_pv = instr_desc(128, 1);
+    const uint32_t s_tmem = tmem_u + COL_S + grp * 128, o_tmem = tmem_u + COL_O + grp * 128;
+    const uint64_t adesc_q = smem_desc(base_u + W2C_OFF_Q + grp * kTileBytes, 16, 1024), adesc_q2 = smem_desc(base_u + W2C_OFF_Q + (2 + grp) * kTileBytes, 16, 1024);
+    const uint32_t bar_sfull = bars_u + 8 * (WS_FULL + 2 * grp), bar_pfull = bars_u + 8 * (WP_FULL + 2 * grp);
+    int gbase = 0, ic = 0, cnt_p[2] = {0, 0};          // halves of the items so far; the group's items and P's (by buffer) so far
+    bool ok = true;
+    for (int idx = ib; idx < ie && ok; ++idx) {
+      const DeviceItem it = get_item_w2(c, misc, idx, ib);
+      const int n_pages = it.n_pages, n_halves = (n_pages + 3) >> 2;
+      if (it.n_q_tok > grp * tpt) {
+        const bool both = it.n_q_tok > tpt;
+        auto release = [&](uint32_t bar) {             // (an absent group has its share done here)
+          tc_commit_lane0(bar);
+          if (!both && lane == 0) mbar_arrive(bar);
+        };
+        auto there = [&](int bar, int v) { return wait_all(bars_u + 8 * (bar + (gbase + v) % kStagesW2c), (gbase + v) / kStagesW2c & 1); };
+        auto issue_s = [&](int v) {
+          const int st = (gbase + v) % kStagesW2c;
+          const uint32_t idesc_s = instr_desc((uint32_t)min(4, n_pages - 4 * v) * 16u, 0);
+          const uint64_t kdesc = smem_desc(base_u + W2C_OFF_K + st * kStageW2c, 16, 2048);
+          tc_mma_ss_k128_lane0<kHalf, 1024>(s_tmem + (v & 1) * 64, adesc_q, kdesc, idesc_s);
+          if (c.split_q) tc_mma_ss_k128_lane0<kHalf, 1024, true>(s_tmem + (v & 1) * 64, adesc_q2, kdesc, idesc_s);
+          tc_commit_lane0(bar_sfull + 8 * (v & 1));
+          release(bars_u + 8 * (WK_EMPTY + st));
+        };
+        if (grp == 1) {
+          const long long t0 = clock64();
+          while (ok && __shfl_sync(fm, *lead, 0) < idx) {
+            __nanosleep(100);
+            if (__shfl_sync(fm, (*ab || clock64() - t0 > kWaitCycles) ? 1 : 0, 0)) { *ab = 1; ok = false; }
+          }
+        }
+        ok = ok && wait_all(bars_u + 8 * (WQ_FULL + grp), ic & 1);
+        ++ic;
+        for (int v = 0; v < min(2, n_halves) && ok; ++v) {
+          ok = there(WK_FULL, v);
+          if (!ok) break;
+          tc_fence_after();
+          issue_s(v);
+        }
+        for (int v = 0; v < n_halves && ok; ++v) {
+          const int st = (gbase + v) % kStagesW2c, b = v & 1;
+          // what is usually there is waited for first, so that a half's P is all that its operations still need
+          ok = there(WV_FULL, v) && (v + 2 >= n_halves || there(WK_FULL, v + 2)) && wait_all(bar_pfull + 8 * b, cnt_p[b] & 1);
+          ++cnt_p[b];
+          if (!ok) break;
+          tc_fence_after();
+          tc_mma_ts_pv_lane0<32>(o_tmem, s_tmem + b * 64, smem_desc(base_u + W2C_OFF_V + st * kStageW2c, 1024, 2048), idesc_pv, v > 0 ? 1u : 0u,
+                                 min(4, n_pages - 4 * v));
+          if (v + 2 < n_halves) issue_s(v + 2);
+          if (v == n_halves - 1) tc_commit_lane0(bars_u + 8 * (WO_FULL + grp));
+          release(bars_u + 8 * (WV_EMPTY + st));
+        }
+      }
+      if (grp == 0 && lane == 0) *lead = idx + 1;
+      gbase += n_halves;
+    }
+    if (grp == 0 && lane == 0) *lead = ie;
+    __syncwarp();
   } else {
     // ================================ MMA issuers (warp 10: group 0, warp 11: group 1) ================================
     // One warp per group, one cursor, operations in the order the operands come: the P.V of a half as soon as its P
@@ -744,7 +819,7 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
             tc_fence_after();
             if (lane == 0 && grp == 0) ASPD_STAMP(c, g, 10 + h);
             // 16 keys = one page per k-step
-            tc_mma_ts_pv_lane0<SC & kCapped ? 32 : 16>(o_tmem, s_tmem + h * 64, smem_desc(vbuf + 4 * h * 4096, 1024, 2048), idesc_pv, (t > 0 || h > 0) ? 1u : 0u, min(4, npg - 4 * h));
+            tc_mma_ts_pv_lane0<16>(o_tmem, s_tmem + h * 64, smem_desc(vbuf + 4 * h * 4096, 1024, 2048), idesc_pv, (t > 0 || h > 0) ? 1u : 0u, min(4, npg - 4 * h));
             // (Asked for only when a row's reference moves.  Before the word of the scores behind it, which send the group
             // two halves on, and before O's: a group that waits for half hc - 1 then knows that half hc - 2 is through,
             // and the parity tells the two apart.)
