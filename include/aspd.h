@@ -124,7 +124,8 @@ typedef struct {
   int32_t wide_rows;    /* plans that deal whole streams to the tensor-core kernel: query rows of a row
                            block, 128 (one tile) or 256 (two tiles scored against every K/V tile the CTA
                            fetches); 0 = automatic (256 when a request has more query tokens than one
-                           tile holds).  Always 128 for scores capped above 55 or capped with a bias that raises any  */
+                           tile holds).  Scores capped above 55 or capped with a bias that raises any:
+                           never 256, and cut instead of dealt unless queries come rotated (aspd_scores_t)      */
   int32_t mma_m;        /* stream-K plans of the tensor-core kernel: M of its MMAs, 128 (the at most 64 query
                            rows of a row block are replicated to fill 128 accumulator rows), 64 (half the
                            tensor work; the accumulators then use 16 lanes of each quadrant) or 96, which

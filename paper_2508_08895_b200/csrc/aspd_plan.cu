@@ -690,6 +690,13 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   bool deal_streams = mode == ASPD_MODE_BRANCH && !shared_mask && tune.chunk_tokens == 0 &&
                       (long)streams.size() >= 2L * ctas_for(total_pages) && (tune.n_ctas > 0 || ctas_for(total_pages) >= p->sm_count);
   if (deal_streams && (long)streams.size() < 4L * ctas_for(total_pages)) deal_streams = !coarse && deal_out(ctas_for(total_pages)) <= kDealSkew;
+  // Capped scores of queries that the attention rotates: those come in two pieces, for which the one-tile variant has no room.  Such
+  // streams are dealt to the two-tile kernel or cut.
+  if (deal_streams && cap > 0.f && !rotated && kernel == ASPD_KERNEL_MMA && wide_ok) {
+    int most_q = 0;
+    for (const Block& bk : blocks) most_q = std::max(most_q, bk.n_tok);
+    deal_streams = p->fixed_ref && tune.wide_rows != 128 && (most_q > kMaxRowsWide / G || tune.wide_rows == 256);
+  }
   if (like) deal_streams = like->dealt != 0;
   p->wide = 0;
   if (deal_streams) {
