@@ -101,14 +101,7 @@ def test_saturated_caps(shape, cap, q_scale):
     """Scores far beyond the cap: tanh at its ends."""
     s = Scene(*shape, STEPS["long"], cap=cap, q_scale=q_scale, v_mean=1.0)
     s.step()
-    # a logit's slope is at most 1 and it is at most the cap: what the products are off by is bounded by both
-    got = s.out.double().cpu().numpy()
-    ref, bound = s.reference(**bits(shape), own=2.0 ** -18)
-    weight = np.expm1(2 * cap) if cap < 5 else np.inf
-    assert np.isfinite(got).all()
-    assert (np.abs(got - ref) <= np.minimum(bound, weight + 1)).all()
-    if cap < 5:                          # tighter than the worst case of saturated products: the mean is what the values' mean makes it
-        assert abs(got.mean() - ref.mean()) <= 2e-3
+    s.check(**bits(shape))
 
 
 @pytest.mark.parametrize("shape", [TC, *SMALL[:2], CORES[0]], ids=str)
@@ -164,8 +157,84 @@ def test_updated_plan_in_a_graph():
     assert plan.status() == 0
     later.k_pool, later.v_pool, later.out = s.k_pool, s.v_pool, s.out
     later.check(**bits(TC))
-    with pytest.raises(B.AspdError):
-        scene(TC, DECODE, "rotated").plan(updatable=True).update(DECODE and s.desc, q_pos=np.zeros(s.n, np.int32))
+
+
+def test_refused_updates_leave_the_plan_as_it_is():
+    """q_pos for rotated queries; positions with which the references can no longer be fixed (another kernel instance)."""
+    s = scene(TC, DECODE, "rotated")
+    plan = s.plan(updatable=True)
+    with pytest.raises(B.AspdError) as e:
+        plan.update(s.desc, q_pos=np.zeros(s.n, np.int32))
+    assert e.value.status == -1
+    s.step(plan)
+    s.check(**bits(TC))
+
+    s = scene(TC, [(100, [(20, -1, 100), (7, 1, 300)], 0)], "both")
+    plan = s.plan(updatable=True)
+    later = scene(TC, [(100, [(20, -1, 400), (7, 1, 300)], 0)], "both")       # keys later than the query
+    with pytest.raises(B.AspdError) as e:
+        plan.update(later.desc)
+    assert e.value.status == -3
+    s.step(plan)
+    s.check(**bits(TC))
+    later.step()
+    later.check(**bits(TC))
+
+
+@pytest.mark.parametrize("shape", [TC, SMALL[0], SMALL[1], CORES[0]], ids=str)
+@pytest.mark.parametrize("cap", [1e-3, 54.0, 57.0, 1e4, 1e30])
+def test_the_smallest_and_largest_caps(shape, cap):
+    """Caps around the limit of fixed references, ones that the scores never come near, one that leaves weights all alike."""
+    for step in ("long", "whole"):
+        for kw in (dict(), dict(n_ctas=2)):
+            s = Scene(*shape, STEPS[step], cap=cap, q_scale=5.0)
+            s.step(**kw)
+            s.check(**bits(shape))
+
+
+def test_branches_that_start_at_different_positions_under_the_shared_mask():
+    for shape in (TC, SMALL[0], CORES[0]):
+        s = scene(shape, [(50, [(20, 3), (5, 1, 900), (30, 0, 4), (0, 2)], 0)], "both", mask=B.MASK_SHARED)
+        s.step()
+        s.check(**bits(shape))
+
+
+def test_two_streams_and_a_replayed_graph_of_whole_branches():
+    """The two-tile kernel's instances side by side on two streams, each with a plan of its own; the same, captured and replayed."""
+    import torch
+    scenes = [Scene(*TC, WHOLE, q_scale=5.0, cap=cap, slopes=sl, seed=seed) for cap, sl, seed in ((20.0, None, 1), (30.0, alibi(28), 2))]
+    streams = [torch.cuda.Stream() for _ in scenes]
+    plans = [s.plan(n_ctas=2, stream=st) for s, st in zip(scenes, streams)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, p, st in zip(scenes, plans, streams):
+            B.branch_step(p, s.q, s.k, s.v, s.k_pool, s.v_pool, s.out, stream=st)
+    torch.cuda.synchronize()
+    for s, p in zip(scenes, plans):
+        assert p.status() == 0
+        s.check(**bits(TC))
+        s.out.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for s, p in zip(scenes, plans):
+            B.branch_step(p, s.q, s.k, s.v, s.k_pool, s.v_pool, s.out)
+    for s in scenes:
+        s.q.neg_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for s in scenes:
+        s.check(**bits(TC))
+
+
+def test_a_step_without_queries():
+    s = scene(TC, [(40, [(20, 0), (9, 0)], 0)], "both")
+    plan = s.plan()
+    assert plan.n_new == 0
+    B.branch_step(plan, s.q, s.k, s.v, s.k_pool, s.v_pool, s.out)
+    import torch
+    nm = B.QkNorm(s.shape)
+    B.qk_norm_append(plan, nm, s.q, s.k, s.v, torch.zeros(1, 0, dtype=torch.int32, device="cuda"), s.k_pool, s.v_pool, s.out)
+    torch.cuda.synchronize()
 
 
 @pytest.mark.parametrize("shape", [TC, *SMALL, *CORES], ids=str)
