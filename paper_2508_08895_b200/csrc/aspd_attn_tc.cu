@@ -114,7 +114,7 @@ struct Ctx {
   int G, inv_g;                // query heads of a KV head; 65536 / G rounded up (token_of)
   float scale_log2;            // (1 in the instances for plans with scores of their own)
   ScoreParams sp;              // those instances: what makes logits of the products
-  int split_q;                 // those instances: queries in two bf16 pieces (plans that rotate them)
+  int split_q;                 // capped scores, two-tile kernel: queries in two bf16 pieces (plans that rotate them)
   int early_fetch;             // plan promise: pages without new rows are not written by in-flight work
   int m64;                     // MMAs with M = 64: row blocks of at most 64 rows are not padded to 128 (half the tensor work)
   int pv64;                    // only P.V with M = 64 (scores and the softmax layout stay at M = 128): O then sits in 16 lanes
@@ -154,8 +154,8 @@ __device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
 }
 
 // What the scores of a kernel instance's plans are: the plain products; capped or with a distance bias (score_row); capped with
-// fixed references (softmax_item_fixed).
-enum { kProducts = 0, kScored = 1, kFixed = 2 };
+// fixed references (softmax_item_fixed).  kSplit with either: queries in two pieces (not in the wide variant).
+enum { kProducts = 0, kScored = 1, kFixed = 2, kSplit = 4 };
 
 template <int NC, bool SC>   // NC = padded row count R = columns of a row replica; a thread takes half of them
 __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p,
@@ -746,7 +746,7 @@ __device__ __forceinline__ bool softmax_item_wide(const Ctx& c, const DeviceItem
 // A operand.  Called by NT threads (rank 0 .. NT - 1); all loads of a thread's rows are issued
 // before the first use.  Unit e = (row e / 8, 16-byte chunk e % 8 of each span); a call covers
 // units e0 + rank + NT u, u < U (row blocks of 64 rows have 512 units, of 128 rows 1024).
-// SPLIT: with what the rounding left over as a second tile (plans with scores of their own, where c.split_q): such scores are large -- a cap
+// SPLIT: with what the rounding left over as a second tile (plans with scores of their own that rotate the queries): such scores are large -- a cap
 // is for those -- and a logit is off by what the rounding takes from a product.  Logits with a deviation of 5: outputs off from 64 bits by
 // 0.0045 (relative, root mean square) with queries rounded to bf16, 0.0024 in two pieces, 0.0017 of it by the output's own rounding.
 template <int U, bool SPLIT = false>
@@ -813,12 +813,10 @@ __device__ __forceinline__ void prep_q_store(const Ctx& c, const DeviceItem& it,
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kHalf), "r"(qu.hi[u][0]), "r"(qu.hi[u][1]), "r"(qu.hi[u][2]),
                    "r"(qu.hi[u][3]) : "memory");
       if constexpr (SPLIT) {
-        if (c.split_q) {
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kTileBytes), "r"(qu.lo2[u][0]), "r"(qu.lo2[u][1]), "r"(qu.lo2[u][2]),
-                       "r"(qu.lo2[u][3]) : "memory");
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kTileBytes + kHalf), "r"(qu.hi2[u][0]), "r"(qu.hi2[u][1]), "r"(qu.hi2[u][2]),
-                       "r"(qu.hi2[u][3]) : "memory");
-        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kTileBytes), "r"(qu.lo2[u][0]), "r"(qu.lo2[u][1]), "r"(qu.lo2[u][2]),
+                     "r"(qu.lo2[u][3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr + kTileBytes + kHalf), "r"(qu.hi2[u][0]), "r"(qu.hi2[u][1]), "r"(qu.hi2[u][2]),
+                     "r"(qu.hi2[u][3]) : "memory");
       }
     }
   }
@@ -929,13 +927,13 @@ __device__ __forceinline__ bool patch_tile(uint32_t base, uint32_t bars, volatil
 //              narrow row blocks
 //   kPatch     kPlain for fused steps of plans that patch their tiles (patch_tile)
 enum { kPlain = 0, kOptions = 1, kPatch = 2 };
-// SCORES: kProducts, kScored or kFixed.
+// SCORES: kProducts; kScored or kFixed, with kSplit or not.
 template <bool WIDE, int MODE, int SCORES>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
   constexpr bool OPT = MODE == kOptions, PATCH = MODE == kPatch, SC = SCORES != kProducts;
   // the second piece of the queries lies where the next item's tile would be; then, as in the wide variant, there is one query tile
-  constexpr bool SPLIT = SC && !WIDE;
-  const bool one_q = WIDE || (SPLIT && c.split_q);
+  constexpr bool SPLIT = (SCORES & kSplit) != 0, ONE_Q = WIDE || SPLIT;
+  static_assert(!(WIDE && SPLIT), "there is no room for the second tile");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -1023,7 +1021,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const uint32_t p = base + OFF_P;
       if (WIDE && M > 64) {
         if constexpr (WIDE) ok = softmax_item_wide<SC>(c, it, misc, bars, p, tmem, item_no, g);
-      } else if constexpr (SCORES == kFixed) {
+      } else if constexpr ((SCORES & kFixed) != 0) {
         ok = M <= 32 ? softmax_item_fixed<32>(c, it, misc, bars, p, tmem, item_no, g) : softmax_item_fixed<64>(c, it, misc, bars, p, tmem, item_no, g);
       } else {
         bool scores64 = false;                     // scores with M = 64 (plans with scores of their own never have them)
@@ -1132,7 +1130,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const uint32_t base_u = __shfl_sync(full_mask, base, 0), bars_u = base_u + off_misc;
       struct TileRef { int npg, first, last, qb, ob, item_no, fresh; };   // qb: query tile (always 0 where there is one); fresh:
                                                                           // 1 + number among the slot's tiles with new rows (0: none)
-      auto q_fill = [one_q](int item_no) { return one_q ? item_no : item_no >> 1; };   // how often the item's query tile was filled before
+      auto q_fill = [](int item_no) { return ONE_Q ? item_no : item_no >> 1; };   // how often the item's query tile was filled before
       auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(full_mask, mbar_wait(bar, parity, ab)) != 0; };
       const uint32_t mma_m = OPT && c.m64 ? 64u : 128u;
       const uint32_t idesc_pv = instr_desc(128, 1, ((OPT && c.m64) || c.pv64) ? 64u : 128u);
@@ -1155,10 +1153,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
         const uint32_t idesc_s = instr_desc((uint32_t)tr.npg * 16u, 0, mma_m);
         // k-step ks covers head_dim elements [16 ks, 16 ks + 16): span ks / 4, 32 bytes per step
         tc_mma_ss_k128_lane0<kHalf, 1024>(tmem_u + COL_S + sb * 128, smem_desc(qbuf, 16, 1024), smem_desc(kbuf, 16, 2048), idesc_s);
-        if constexpr (SPLIT) {
-          if (c.split_q)
-            tc_mma_ss_k128_lane0<kHalf, 1024, true>(tmem_u + COL_S + sb * 128, smem_desc(qbuf + kTileBytes, 16, 1024), smem_desc(kbuf, 16, 2048), idesc_s);
-        }
+        if constexpr (SPLIT)
+          tc_mma_ss_k128_lane0<kHalf, 1024, true>(tmem_u + COL_S + sb * 128, smem_desc(qbuf + kTileBytes, 16, 1024), smem_desc(kbuf, 16, 2048), idesc_s);
         if (lane == 0) ASPD_STAMP(c, g, 9);
         tc_commit_lane0(bars_u + 8 * (S_FULL + sb));
         tc_commit_lane0(bars_u + 8 * (K_EMPTY + sb));
@@ -1190,7 +1186,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       for (int idx = ib; idx < ie && ok; ++idx, ++item_no) {
         const int n_pages = get_item(c, misc, idx, ib).n_pages, n_tiles = (n_pages + 7) >> 3;
         for (int t = 0; t < n_tiles && ok; ++t, ++g) {
-          TileRef cur = {min(8, n_pages - t * 8), t == 0, t == n_tiles - 1, one_q ? 0 : item_no & 1, item_no & 1, item_no, 0};
+          TileRef cur = {min(8, n_pages - t * 8), t == 0, t == n_tiles - 1, ONE_Q ? 0 : item_no & 1, item_no & 1, item_no, 0};
           ok = issue_s(cur, g);
           if (ok && have_prev) ok = issue_pv(prev, g - 1);
           prev = cur;
@@ -1223,8 +1219,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
       const int ob = item_no & 1, M = it.n_q_tok * G, R = M <= 32 ? 32 : (M <= 64 ? 64 : 128),
                 KS = ((OPT && c.m64) ? 64 : 128) / R;                // replicas in the softmax threads' layout
       if (idx + 1 < item_end) {                    // the next item's query tile: into the other buffer, or (wide
-        const int qn = one_q ? 0 : (item_no + 1) & 1;   // kernel) into the only one once this item's last S is issued
-        const int fills = one_q ? item_no + 1 : (item_no + 1) >> 1;
+        const int qn = ONE_Q ? 0 : (item_no + 1) & 1;   // kernel) into the only one once this item's last S is issued
+        const int fills = ONE_Q ? item_no + 1 : (item_no + 1) >> 1;
         if constexpr (WIDE) {
           // the only query tile is free once this item's last S has been issued: rotate the next
           // item's rows into registers first, so that only the stores are left for after the wait
@@ -1240,7 +1236,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(Ctx c) {
           QUnits<4, true> q0;
           prep_q_compute<128, 4, true>(c, nx, et, 0, q0);
           dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
-          prep_q_store<128, 4, true>(c, nx, base + OFF_Q + qn * kTileBytes, et, 0, q0);
+          prep_q_store<128, 4, true>(c, nx, base + OFF_Q, et, 0, q0);
         } else {
           dead |= !mbar_wait(bars + 8 * (Q_EMPTY + qn), (fills & 1) ^ 1, ab);
           prep_q(c, get_item(c, misc, idx + 1, item_begin), base + OFF_Q + qn * kTileBytes, et);
@@ -1438,11 +1434,14 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
     };
     auto all = [&](auto scores) {
       constexpr int S = decltype(scores)::value;
-      return attr(attn_tc_kernel<false, kPlain, S>, kSmemBytes) && attr(attn_tc_kernel<false, kOptions, S>, kSmemBytes) &&
-             attr(attn_tc_kernel<false, kPatch, S>, kSmemBytes) && attr(attn_tc_kernel<true, kPlain, S>, kSmemBytes);
+      bool ok = attr(attn_tc_kernel<false, kPlain, S>, kSmemBytes) && attr(attn_tc_kernel<false, kOptions, S>, kSmemBytes) &&
+                attr(attn_tc_kernel<false, kPatch, S>, kSmemBytes);
+      if constexpr (!(S & kSplit)) ok = ok && attr(attn_tc_kernel<true, kPlain, S>, kSmemBytes);
+      return ok;
     };
     if (!all(std::integral_constant<int, kProducts>()) || !all(std::integral_constant<int, kScored>()) ||
-        !all(std::integral_constant<int, kFixed>()) || !attr(attn_tc_w2_kernel<kPlainScores>, kSmemBytesW2) ||
+        !all(std::integral_constant<int, kFixed>()) || !all(std::integral_constant<int, kScored | kSplit>()) ||
+        !all(std::integral_constant<int, kFixed | kSplit>()) || !attr(attn_tc_w2_kernel<kPlainScores>, kSmemBytesW2) ||
         !attr(attn_tc_w2_kernel<kCapped>, kSmemBytesW2) || !attr(attn_tc_w2_kernel<kBiased>, kSmemBytesW2) ||
         !attr(attn_tc_w2_kernel<kCapped | kBiased>, kSmemBytesW2))
       return ASPD_ERR_CUDA;
@@ -1486,12 +1485,13 @@ static int launch_tc(const aspd_plan* p, const void* q, const void* k_new, const
   }
   auto instance = [&](auto scores) {
     constexpr int S = decltype(scores)::value;
-    return p->wide ? attn_tc_kernel<true, kPlain, S>
+    return p->wide ? attn_tc_kernel<true, kPlain, S & ~kSplit>
            : c.m64 || c.merge_out != nullptr || c.out != nullptr ? attn_tc_kernel<false, kOptions, S>
            : c.k_new != nullptr && p->patch_tiles ? attn_tc_kernel<false, kPatch, S> : attn_tc_kernel<false, kPlain, S>;
   };
   auto* kernel = !p->scored() ? instance(std::integral_constant<int, kProducts>())
-                 : p->fixed_ref ? instance(std::integral_constant<int, kFixed>()) : instance(std::integral_constant<int, kScored>());
+                 : p->rotated ? (p->fixed_ref ? instance(std::integral_constant<int, kFixed>()) : instance(std::integral_constant<int, kScored>()))
+                 : p->fixed_ref ? instance(std::integral_constant<int, kFixed | kSplit>()) : instance(std::integral_constant<int, kScored | kSplit>());
   const cudaError_t e = launch_pdl(kernel, dim3(p->n_ctas), dim3(kThreads), kSmemBytes, s, c);
   return e == cudaSuccess ? ASPD_OK : ASPD_ERR_CUDA;
 }
