@@ -88,7 +88,8 @@ typedef struct {
                         request's prefix_len plus the kv_len of all its ASPD_Q_SHARED regions, the same
                         for every branch of the stage (branches share the ID of a timestep).  Any
                         value >= 0 is taken as given (position-ID variants of the ablation).  Ignored
-                        for ASPD_Q_SHARED regions and in serial mode.                              */
+                        for ASPD_Q_SHARED regions and in serial mode, unless the plan has a distance
+                        bias (aspd_scores_t).                                                      */
   int32_t q_len;     /* query tokens this step = the LAST q_len tokens (0: finished branch of the
                         current stage, invisible to the other branches; ASPD_Q_SHARED: region of an
                         earlier stage, visible to every branch -- Eq. 3, different stages)       */
@@ -113,8 +114,8 @@ typedef struct {
                            such a plan serves aspd_plan_info / aspd_plan_items only        */
   int32_t stable_cache; /* 1: the caller promises that, when an attention call of this plan is
                            made, nothing still in flight on the stream writes K/V pages the plan
-                           reads, except this step's own new rows (written by aspd_kv_append with
-                           this plan, or by the fused step).  True for a decode loop, where a
+                           reads, except this step's own new rows (written by aspd_kv_append or
+                           aspd_qk_norm_append with this plan, or by the fused step).  True for a decode loop, where a
                            layer's pools are only touched by that layer's own step.  The kernel
                            may then start fetching such pages before the previous kernel on the
                            stream has finished.  0 (default): full stream ordering for the pools */
