@@ -267,8 +267,8 @@ typedef struct {
   const float* slopes; /* host [n_q_heads], read before the call returns; NULL: no bias         */
   int32_t rotated;     /* 1: q and k_new come as they are to be used (aspd_qk_norm_append with rotate_q, or a model
                           without rotation): the attention and the fused step rotate nothing (the plan's q_pos are all
-                          0; a caller's are refused).  Their elements must be finite.  aspd_kv_append still rotates by
-                          the positions it is given                                                     */
+                          0; a caller's are refused; aspd_step_host takes its pos for read).  Their elements must be finite.
+                          aspd_kv_append still rotates by the positions it is given                     */
 } aspd_scores_t;
 /*
  * aspd_plan_create with these options (scores = NULL: the same).  ASPD_ERR_INVALID_ARG for a cap that is

@@ -1431,7 +1431,7 @@ int aspd_step_host_async(aspd_plan_t* p, const void* q, const void* k_new, const
     return ASPD_ERR_CUDA;
   }
   int rc;
-  if (memcmp(pos, p->q_pos.data(), sizeof(int32_t) * p->n_new) == 0) {
+  if (p->rotated || memcmp(pos, p->q_pos.data(), sizeof(int32_t) * p->n_new) == 0) {
     // the caller's position IDs are the plan's (the usual case): they are on the device already,
     // and the step may write the new rows inside the attention pass
     rc = run_step(p, p->mode, p->dev.st_q, p->dev.st_k, p->dev.st_v, k_pool, v_pool, p->dev.st_out, stream);

@@ -128,7 +128,7 @@ def test_calls_apart_host_step_static_and_graph(shape):
         s.k_pool, s.v_pool = (x.clone() for x in pools)
         host = [x.cpu().pin_memory() for x in (s.q, s.k, s.v)]
         out = torch.zeros_like(host[0]).pin_memory()
-        B.step_host(plan, *host, pos.copy(), s.k_pool, s.v_pool, out)
+        B.step_host(plan, *host, B.positions(s.desc, s.mode)[0].copy(), s.k_pool, s.v_pool, out)      # (rotated: whatever they are)
         s.out.copy_(out)
         assert same()
 
@@ -197,6 +197,32 @@ def test_branches_that_start_at_different_positions_under_the_shared_mask():
         s = scene(shape, [(50, [(20, 3), (5, 1, 900), (30, 0, 4), (0, 2)], 0)], "both", mask=B.MASK_SHARED)
         s.step()
         s.check(**bits(shape))
+
+
+@pytest.mark.parametrize("shape", [TC, SMALL[1], CORES[1]], ids=str)
+def test_pages_beyond_four_gigabytes(shape):
+    """Pools whose byte offsets pass 32 bits: the same step with its pages at their far ends, norms and all."""
+    import torch
+    near = Scene(*shape, OPEN, cap=20.0, slopes=alibi(shape[3][0]), rotated=True, q_scale=5.0)
+    page = B.pool_bytes(near.shape, 1)
+    n_pool = (9 << 29) // page + near.n_pool                      # 4.5 GiB and a step
+    dt = near.q.dtype
+    pools = [torch.zeros(n_pool * page // near.q.element_size(), dtype=dt, device="cuda") for _ in "kv"]
+    first = n_pool - near.n_pool
+    for big, small in zip(pools, (near.k_pool, near.v_pool)):
+        big[first * page // near.q.element_size():] = small
+    far = dict(near.desc, page_ids=near.desc["page_ids"] + np.int32(first))
+    plan = B.Plan(near.shape, far, n_pool, near.mode, scores=near.scores)
+    nm = B.QkNorm(near.shape, torch.ones(near.d, dtype=dt, device="cuda"), None, 1e-6)
+    pos = torch.from_numpy(B.positions(far, near.mode)[0].copy()).cuda()
+    q = near.q.clone()
+    B.qk_norm_append(plan, nm, q, near.k, near.v, pos, *pools, near.q)
+    B.branch_attn(plan, near.q, *pools, near.out)
+    torch.cuda.synchronize()
+    assert plan.status() == 0
+    near.k_pool, near.v_pool = (big[first * page // near.q.element_size():].clone() for big in pools)
+    assert all(not big[:first * page // near.q.element_size()].any() for big in pools)
+    near.check(**bits(shape))
 
 
 def test_two_streams_and_a_replayed_graph_of_whole_branches():
