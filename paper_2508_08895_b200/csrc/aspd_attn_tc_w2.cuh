@@ -40,7 +40,7 @@ template <int SCORES> constexpr int kThreadsW2 = (kSoftmaxWarpsW2<SCORES> + 4) *
 constexpr uint32_t W2_OFF_K = 0, W2_OFF_V = 2 * kTileBytes, W2_OFF_Q = 4 * kTileBytes, W2_OFF_OUT = 6 * kTileBytes,
                    W2_OFF_MISC = 7 * kTileBytes;
 constexpr size_t kSmemBytesW2 = 7 * kTileBytes + 2048 + 1024;   // + Misc + slack to align the base to 1024
-constexpr int kItemCacheW2 = 7;
+constexpr int kItemCacheW2 = 30;
 // Capped scores (softmax_group_capped): a stage of K or V is 64 keys, three of either, and a group has two query tiles, the second with what
 // the rounding of the first left over (QUnits).
 constexpr int kStagesW2c = 3;
@@ -64,7 +64,6 @@ struct MiscW2 {
   int abort_flag;
   int lead;                          // the item group 0's issuer is at (read by group 1's)
   int kpos[kPageRingW2][8];          // plans with a distance bias: position IDs of the pages' first rows (ring as nval)
-  float lsum[2][128];                // capped scores, per group: where a row's two sums meet
 };
 static_assert(sizeof(MiscW2) <= 2048, "MiscW2 must fit behind the tiles");
 
@@ -432,12 +431,29 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
   const uint32_t qbuf = base + W2C_OFF_Q + grp * kTileBytes;
   const uint32_t bar_sfull = bars + 8 * (WS_FULL + 2 * grp), bar_pfull = bars + 8 * (WP_FULL + 2 * grp),      // + 8 h
                  bar_ofull = bars + 8 * (WO_FULL + grp), bar_qfull = bars + 8 * (WQ_FULL + grp);
+  // the first item from `idx` on in which the group has a tile: its query tile is prepared, what its row may see asked for, and the
+  // queries of the item behind it called into L2
+  int4 vis = make_int4(0, 0, 0, 0);
+  RowBias rb = {0.f, 0};
   auto next_item = [&](int idx) {
     for (; idx < item_end; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, item_begin);
-      if (it.n_q_tok > grp * tpt) {
-        prep_tile_w2<256, true>(c, it.q_tok0 + grp * tpt, min(tpt, it.n_q_tok - grp * tpt), it.kv_head, qbuf, tid & 255);
+      const int n_tok = min(tpt, it.n_q_tok - grp * tpt);
+      if (n_tok > 0) {
+        prep_tile_w2<256, true>(c, it.q_tok0 + grp * tpt, n_tok, it.kv_head, qbuf, tid & 255);
         warp_arrive_w2(bar_qfull);
+        const int tl = token_of(c, r), tok = it.q_tok0 + grp * tpt + tl;
+        vis = make_int4(0, 0, 0, 0);                           // padding rows see nothing
+        rb = {0.f, 0};
+        if (r < n_tok * G) {
+          vis = c.pd.tok_vis[tok];
+          if (BIAS) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
+        }
+        if (idx + 1 < item_end) {
+          const DeviceItem nx = get_item_w2(c, misc, idx + 1, item_begin);
+          if (r < (nx.n_q_tok - grp * tpt) * G)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(c.q + ((size_t)(nx.q_tok0 + grp * tpt + tl) * c.n_q_heads + nx.kv_head * G + r - tl * G) * 128 + part * 64));
+        }
         break;
       }
     }
@@ -451,10 +467,6 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
     const int n_tok = min(tpt, it.n_q_tok - grp * tpt);
     if (n_tok <= 0) { g += n_halves; continue; }               // the block has no second tile
     const int tl = token_of(c, r), M = n_tok * G, tok = it.q_tok0 + grp * tpt + tl;
-    int4 vis = make_int4(0, 0, 0, 0);                          // padding rows see nothing
-    RowBias rb = {0.f, 0};
-    if (r < M) vis = c.pd.tok_vis[tok];
-    if (BIAS && r < M) rb = row_bias(c.pd, tok, it.kv_head * G + r - tl * G);
     float l = 0.f;
     bool far = false;                                           // the warp's last half had scores beyond the short polynomial
     for (int t = 0; t < n_halves; ++t, ++g) {
@@ -532,15 +544,18 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
         warp_arrive_w2(bar_pfull + 8 * h);
       }
     }
-    // ---- the next query tile, beside the rest of this item; then the row's two sums meet, and each of its threads
-    // normalises and stores half of it (there is no room left to bring eight lanes' 16 bytes together; the stores are 4 % of
-    // a long item's lines)
+    // ---- The row's two sums meet in tensor memory, in columns of the group's first buffer that hold neither P nor scores to come (those of the
+    // next item wait for its queries); the only barrier of an item.
+    tmem_st1(s_base + 20, l);
+    tmem_wait_st();
+    tc_fence_before();
+    if (named_sync_or(1 + grp, 256, dead || *ab)) break;
+    tc_fence_after();
+    l += tmem_ld1(s_base + (part ? -12 : 52));
+    tc_fence_before();
+    // ---- the next query tile, beside the last P.V; then each of the row's threads normalises and stores half of it (there is no room left to
+    // bring eight lanes' 16 bytes together)
     next_item(idx + 1);
-    if (part == 1) misc->lsum[grp][r] = l;
-    named_sync(1 + grp, 256);
-    if (part == 0) misc->lsum[grp][r] += l;
-    named_sync(1 + grp, 256);
-    l = misc->lsum[grp][r];
     dead |= !mbar_wait(bar_ofull, ic & 1, ab);
     tc_fence_after();
     ++ic;
@@ -559,7 +574,6 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
       }
     }
     tc_fence_before();
-    if (named_sync_or(1 + grp, 256, dead || *ab)) break;
   }
 }
 

@@ -248,6 +248,16 @@ __device__ __forceinline__ void tmem_wait_ld16(float (&v)[16]) {
 __device__ __forceinline__ void tmem_wait_ld32(float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : ASPD_RW8(v, 0), ASPD_RW8(v, 8), ASPD_RW8(v, 16), ASPD_RW8(v, 24)::"memory");
 }
+// one column of this thread's TMEM lane
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {      // (waits for the load)
+  float v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=f"(v) : "r"(taddr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v) :: "memory");
+  return v;
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared-memory matrix descriptor, 128-byte swizzle, descriptor version 1.
