@@ -362,6 +362,9 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
 
 // The same for capped scores with fixed references (aspd_plan::fixed_ref): no maximum, nothing exchanged, nothing taken twice, and the
 // scores' columns are free as soon as they are in registers.
+// A row is divided by the sum of its weights as P.V takes them, rounded to bf16: a row's largest weight is not 1 here, which bf16 holds
+// exactly, and where it is nearly all of the sum its rounding would be the output's.  Outputs off from 64 bits (relative, root mean square; 0.0017 is
+// their own rounding): logits with a deviation of 5, 0.0019, of 9, 0.0016 to 0.0017; with the sum of unrounded weights 0.0023, and 0.0022 to 0.0029.
 // With moving references and this one, us a layer: one request of 2 k tokens 7.6 and 7.1 (plain scores 7.2), 32 requests 47.5 and
 // 46.9 (46.7), the same with scores beyond 0.6 of a cap of 20 58 and 48.
 template <int NC>
@@ -404,6 +407,7 @@ __device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceIte
     score_row(s, c.sp, biased, rb, &misc->kpos[g & 3][col0 / 16]);
     tc_fence_before();
     mbar_arrive(bars + 8 * (S_EMPTY + sb));       // the scores and the tile's entries are not needed again
+    uint32_t pk[HC / 2];
     float2 lsum = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < HC; i += 2) {
@@ -412,9 +416,8 @@ __device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceIte
         x.x = (mask[i / 16] >> (i & 15)) & 1u ? x.x : -INFINITY;
         x.y = (mask[i / 16] >> ((i & 15) + 1)) & 1u ? x.y : -INFINITY;
       }
-      x.x = ex2(x.x); x.y = ex2(x.y);
-      s[i] = x.x; s[i + 1] = x.y;
-      lsum = __fadd2_rn(lsum, x);
+      pk[i / 2] = pack_bf16(ex2(x.x), ex2(x.y));
+      lsum = __fadd2_rn(lsum, unpack_bf16(pk[i / 2]));
     }
     l += lsum.x + lsum.y;
     if (g > 0) dead |= !mbar_wait(bars + 8 * P_EMPTY, (g - 1) & 1, ab);   // P tile is free again
@@ -422,9 +425,8 @@ __device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceIte
     for (int c8 = 0; c8 < HC / 8; ++c8) {
       const int kk = col0 + c8 * 8;
       const uint32_t addr = smem_p + (kk >> 6) * kHalf + r * 128 + ((((kk & 63) >> 3) ^ (r & 7)) << 4);
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(pack_bf16(s[c8 * 8 + 0], s[c8 * 8 + 1])),
-                   "r"(pack_bf16(s[c8 * 8 + 2], s[c8 * 8 + 3])), "r"(pack_bf16(s[c8 * 8 + 4], s[c8 * 8 + 5])),
-                   "r"(pack_bf16(s[c8 * 8 + 6], s[c8 * 8 + 7])) : "memory");
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(pk[c8 * 4]), "r"(pk[c8 * 4 + 1]), "r"(pk[c8 * 4 + 2]), "r"(pk[c8 * 4 + 3])
+                   : "memory");
     }
     fence_async_smem();
     tc_fence_before();
@@ -748,7 +750,8 @@ __device__ __forceinline__ bool softmax_item_wide(const Ctx& c, const DeviceItem
 // units e0 + rank + NT u, u < U (row blocks of 64 rows have 512 units, of 128 rows 1024).
 // SPLIT: with what the rounding left over as a second tile (plans with scores of their own that rotate the queries): such scores are large -- a cap
 // is for those -- and a logit is off by what the rounding takes from a product.  Logits with a deviation of 5: outputs off from 64 bits by
-// 0.0045 (relative, root mean square) with queries rounded to bf16, 0.0024 in two pieces, 0.0017 of it by the output's own rounding.
+// 0.0045 (relative, root mean square) with queries rounded to bf16, 0.0024 in two pieces (0.0019 with what softmax_item_fixed sums), 0.0017 of it by
+// the output's own rounding.
 template <int U, bool SPLIT = false>
 struct QUnits {
   uint32_t lo[U][4], hi[U][4];   // per unit: the rotated chunk of the first and of the second span, bf16 pairs

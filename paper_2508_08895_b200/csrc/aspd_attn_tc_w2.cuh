@@ -402,10 +402,8 @@ __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, co
         x = __ffma2_rn(make_float2(rb.slope, rb.slope), dist, x);
         dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
       }
-      x.x = ex2((mask >> i) & 1u ? x.x : -INFINITY);
-      x.y = ex2((mask >> (i + 1)) & 1u ? x.y : -INFINITY);
-      sum = __fadd2_rn(sum, x);
-      p8[i >> 1] = pack_bf16(x.x, x.y);
+      p8[i >> 1] = pack_bf16(ex2((mask >> i) & 1u ? x.x : -INFINITY), ex2((mask >> (i + 1)) & 1u ? x.y : -INFINITY));
+      sum = __fadd2_rn(sum, unpack_bf16(p8[i >> 1]));
     }
     ASPD_TMEM_ST8U(s_addr + q * 8, p8);
   }
@@ -414,12 +412,12 @@ __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, co
 
 // Capped scores, with fixed references only (aspd_plan::fixed_ref): the exponentials are taken against 0 always, so that nothing but the
 // sums goes from key to key, and a row is two threads': eight warps to a group, thread (part, r) takes 32 of the 64 scores of
-// a half.  17 k query tokens of 32 requests, a cap of 50, us a layer below the power cap: 770 with queries that come rotated (plain scores 690 to
-// 730), 990 with queries in two pieces, whose scores are two products each; the tensor pipe is busy half of the time, the rest is
+// a half.  17 k query tokens of 32 requests, a cap of 50, us a layer below the power cap: 815 with queries that come rotated (plain scores 690 to
+// 730), 1 010 with queries in two pieces, whose scores are two products each; the tensor pipe is busy half of the time, the rest is
 // the way from a half's scores to its P.V.  (Four warps a group, a thread to a row as in softmax_group_w2: 853 instead of 834 under the cap.
 // Two pieces: scores of a whole tile in one product, 1 080 against 1 020 then; the first piece in tensor memory and one buffer of 64 scores, 1 350.)  A half is one pass with the short polynomial, which keeps the largest product; where that turns
 // out to be beyond the polynomial's range (scores above 0.6 of the cap) it is taken again by far_scores, and the warp's next half goes
-// there at once.  P lies over the thread's own scores: 16 columns at columns 0 and 32 of the half's 64.
+// there at once.  Rows are divided by the sum of their rounded weights (see softmax_item_fixed; 2 to 5 % of the time).  P lies over the thread's own scores: 16 columns at columns 0 and 32 of the half's 64.
 template <bool BIAS>
 __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                      int item_end, int grp, int tpt) {
@@ -517,10 +515,10 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
                 x.x = (mask >> i) & 1u ? x.x : -INFINITY;
                 x.y = (mask >> (i + 1)) & 1u ? x.y : -INFINITY;
               }
-              x.x = ex2(x.x); x.y = ex2(x.y);
-              if (i & 2) sum1 = __fadd2_rn(sum1, x);
-              else sum0 = __fadd2_rn(sum0, x);
-              pk[pg * 8 + (i >> 1)] = pack_bf16(x.x, x.y);
+              const uint32_t w = pack_bf16(ex2(x.x), ex2(x.y));
+              if (i & 2) sum1 = __fadd2_rn(sum1, unpack_bf16(w));
+              else sum0 = __fadd2_rn(sum0, unpack_bf16(w));
+              pk[pg * 8 + (i >> 1)] = w;
             }
           }
           sum0 = __fadd2_rn(sum0, sum1);
