@@ -466,13 +466,16 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
   std::vector<int2> visit;
   std::vector<int32_t> page_pos;                      // plans with a distance bias: position ID of every entry's first row
   std::vector<Block> blocks;
-  // Position ID of the first token of a region that is not the prefix (plans with a distance bias).
-  auto region_start = [&](const aspd_request_t& q, const aspd_branch_t& x) -> long {
-    if (x.pos_start != ASPD_POS_AUTO) return x.pos_start;
-    long s = q.prefix_len;
-    for (int b = 0; b < q.n_branches; ++b)
-      if (br[q.branch_begin + b].q_len == ASPD_Q_SHARED) s += br[q.branch_begin + b].kv_len;
-    return s;
+  // Position ID of the first token of a region of request r that is not the prefix; plans without a distance bias do not need it.
+  // A stage's start counts every region before it: once a request, not once a region.
+  std::vector<long> stage_start(biased ? n_req : 0);
+  for (int r = 0; biased && r < n_req; ++r) {
+    stage_start[r] = req[r].prefix_len;
+    for (int b = 0; b < req[r].n_branches; ++b)
+      if (br[req[r].branch_begin + b].q_len == ASPD_Q_SHARED) stage_start[r] += br[req[r].branch_begin + b].kv_len;
+  }
+  auto region_start = [&](int r, const aspd_branch_t& x) -> long {
+    return !biased ? 0 : x.pos_start != ASPD_POS_AUTO ? x.pos_start : stage_start[r];
   };
   bool falling = true;                                // the bias raises no logit
   for (int h = 0; biased && h < Hq; ++h) falling = falling && scores->slopes[h] >= 0.f;
@@ -482,9 +485,9 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
     for (int b = 0; b < req[r].n_branches; ++b) {
       const aspd_branch_t& x = br[req[r].branch_begin + b];
       if (x.kv_len > 0 && x.q_len == ASPD_Q_SHARED && x.pos_start == ASPD_POS_AUTO) { delete p; return ASPD_ERR_BAD_DESCRIPTOR; }
-      if (region_start(req[r], x) + x.kv_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
-      if (x.kv_len > 0 && (mode == ASPD_MODE_SERIAL || x.q_len == ASPD_Q_SHARED)) last_seen = std::max(last_seen, region_start(req[r], x) + x.kv_len - 1);
-      if (shared_mask && x.q_len >= 0) falling = falling && region_start(req[r], x) == region_start(req[r], br[req[r].branch_begin]);
+      if (region_start(r, x) + x.kv_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
+      if (x.kv_len > 0 && (mode == ASPD_MODE_SERIAL || x.q_len == ASPD_Q_SHARED)) last_seen = std::max(last_seen, region_start(r, x) + x.kv_len - 1);
+      if (shared_mask && x.q_len >= 0) falling = falling && region_start(r, x) == region_start(r, br[req[r].branch_begin]);
       total += x.kv_len;
     }
     if (total + req[r].tail_len > kMostBiasPos) { delete p; return ASPD_ERR_TOO_LARGE; }
@@ -538,11 +541,12 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
         std::reverse(page_pos.begin() + at, page_pos.end());
       }
     };
-    auto push_shared = [&](const aspd_request_t& q) {            // prefix and regions of earlier stages: seen by every branch
+    auto push_shared = [&](int r) {                              // prefix and regions of earlier stages: seen by every branch
+      const aspd_request_t& q = req[r];
       push_prefix(q);
       for (int b = 0; b < q.n_branches; ++b) {
         const aspd_branch_t& x = br[q.branch_begin + b];
-        if (x.q_len == ASPD_Q_SHARED) push_region(q, x.kv_off, x.kv_len, x.kv_len, 0, region_start(q, x));
+        if (x.q_len == ASPD_Q_SHARED) push_region(q, x.kv_off, x.kv_len, x.kv_len, 0, region_start(r, x));
       }
     };
     for (int r = 0; r < n_req; ++r) {
@@ -559,13 +563,13 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
         if (nq == 0) continue;
         kv_count += kv_req;
         if (block_tok == 0) {
-          push_shared(q);
+          push_shared(r);
           const int pe = ((int)visit.size() - v0) * ps;
           for (int b = 0; b < q.n_branches; ++b) {
             const aspd_branch_t& x = br[q.branch_begin + b];
             if (x.q_len < 0 || (x.q_len == 0 && !shared_mask)) continue;     // shared mask: also branches without queries
             const int lo = ((int)visit.size() - v0) * ps, prior = x.kv_len - x.q_len;
-            push_region(q, x.kv_off, x.kv_len, prior, t, region_start(q, x), true);
+            push_region(q, x.kv_off, x.kv_len, prior, t, region_start(r, x), true);
             for (int i = 0; i < x.q_len; ++i) tok_vis[t++] = make_int4(pe, lo, lo + prior + i + 1, shared_mask ? prior + i : 0);
           }
           blocks.push_back({r, t_req, nq, v0, (int)visit.size() - v0});
@@ -574,7 +578,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
           for (int blk0 = 0; blk0 < nq; blk0 += block_tok) {
             const int blk1 = std::min(nq, blk0 + block_tok), bv0 = (int)visit.size();
             if (blk0 == 0) {
-              push_shared(q);
+              push_shared(r);
               n_shared = (int)visit.size() - bv0;
             } else {                                           // as in the request's first block
               visit.resize((size_t)bv0 + n_shared);
@@ -592,7 +596,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
               const int a = std::max(blk0, off), e = std::min(blk1, off + x.q_len);
               if (a < e) {
                 const int lo = ((int)visit.size() - bv0) * ps, prior = x.kv_len - x.q_len;
-                push_region(q, x.kv_off, prior + (e - off), prior, t_req + off, region_start(q, x));   // up to the run's last token of this branch
+                push_region(q, x.kv_off, prior + (e - off), prior, t_req + off, region_start(r, x));   // up to the run's last token of this branch
                 for (int i = a - off; i < e - off; ++i) tok_vis[t_req + off + i] = make_int4(pe, lo, lo + prior + i + 1, 0);
               }
               off += x.q_len;
@@ -607,7 +611,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
         long written = q.prefix_len;
         for (int b = 0; b < q.n_branches; ++b) {
           const aspd_branch_t& x = br[q.branch_begin + b];
-          push_region(q, x.kv_off, x.kv_len, x.kv_len, 0, region_start(q, x));
+          push_region(q, x.kv_off, x.kv_len, x.kv_len, 0, region_start(r, x));
           kv_count += x.kv_len; written += x.kv_len;
         }
         push_region(q, q.tail_off, q.tail_len, q.tail_len - 1, t, written);
