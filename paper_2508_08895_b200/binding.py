@@ -384,9 +384,11 @@ def _token_stride(x, dtype, shape) -> int:
 
 def qk_norm_append(plan: Plan, norm: QkNorm, q, k_new, v_new, pos, k_pool, v_pool, q_out, stream=None) -> None:
     """Norms, rotation and paged append of the step's new tokens (see ``aspd_qk_norm_append``).  q, k_new, v_new may be
-    views of one packed projection; pos: device int32 [n_axes][n_new]."""
+    views of one packed projection; pos: device int32 [n_axes][n_new] (further rows are not read; flat: n_axes * n_new)."""
     q_shape, kv_shape, q_size, dtype, int32 = plan._rows()
-    if pos.numel() < norm.n_axes * q_shape[0] or pos.dtype is not int32 or not pos.is_contiguous():
+    n, rows = q_shape[0], pos.shape
+    if not (rows[1] == n and rows[0] >= norm.n_axes if len(rows) == 2 else len(rows) == 1 and rows[0] == norm.n_axes * n) or \
+            pos.dtype is not int32 or not pos.is_contiguous():
         raise ValueError("pos: contiguous int32 [n_axes][n_new]")
     qs, ks, vs = _token_stride(q, dtype, q_shape), _token_stride(k_new, dtype, kv_shape), _token_stride(v_new, dtype, kv_shape)
     if q_out.numel() != q_size or q_out.dtype is not dtype or not q_out.is_contiguous():
