@@ -280,7 +280,7 @@ class Plan:
             import torch
             sh = self.shape
             shapes = [torch.Size((self.n_new, h, sh.head_dim)) for h in (sh.n_q_heads, sh.n_kv_heads)]
-            self._dims = *shapes, shapes[0].numel(), torch.bfloat16 if sh.dtype == DTYPE_BF16 else torch.float32, torch.int32
+            self._dims = *shapes, shapes[0].numel(), _storage_type(sh), torch.int32
         return self._dims
 
     def update(self, desc, q_pos=None, stream=None) -> None:
@@ -361,7 +361,7 @@ class QkNorm:
         if len(axes) != half or not all(0 <= a < MAX_AXES for a in axes):
             raise ValueError(f"axis_of_pair: {half} numbers from 0 to {MAX_AXES - 1}")
         for w in (q_weight, k_weight):
-            if w is not None and (w.numel() != shape.head_dim or not w.is_contiguous() or w.element_size() != _esize(shape)):
+            if w is not None and (w.numel() != shape.head_dim or not w.is_contiguous() or w.dtype is not _storage_type(shape)):
                 raise ValueError("weights: head_dim contiguous elements of the storage type")
         self.weights = q_weight, k_weight           # kept alive
         self.n_axes = max(axes) + 1
@@ -371,6 +371,11 @@ class QkNorm:
 
 def _esize(shape: Shape) -> int:
     return 2 if shape.dtype == DTYPE_BF16 else 4
+
+
+def _storage_type(shape: Shape):
+    import torch
+    return torch.bfloat16 if shape.dtype == DTYPE_BF16 else torch.float32
 
 
 def _token_stride(x, dtype, shape) -> int:

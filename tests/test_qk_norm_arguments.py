@@ -38,3 +38,14 @@ def test_positions_of_several_axes_lie_a_row_of_the_step_apart():
     for axes, rows in ((3, (3, c.n)), (3, (4, c.n)), (3, (3 * c.n,)), (1, (1, c.n)), (1, (c.n,)), (1, (3, c.n))):
         with pytest.raises(B.AspdError):
             c(c.axes(axes), torch.zeros(rows, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype,others", [("bf16", (torch.float16, torch.int16, torch.float32)), ("f32", (torch.int32, torch.bfloat16, torch.float64))])
+def test_gains_are_of_the_storage_type(dtype, others):
+    c = Call(dtype)
+    for other in others:
+        for name in ("q_weight", "k_weight"):
+            with pytest.raises(ValueError):
+                B.QkNorm(c.shape, **{name: torch.ones(64, dtype=other)})
+    with pytest.raises(B.AspdError):
+        c(B.QkNorm(c.shape, torch.ones(64, dtype=c.dt), torch.ones(64, dtype=c.dt)), torch.zeros(1, c.n, dtype=torch.int32))
