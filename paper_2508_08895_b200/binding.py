@@ -274,13 +274,13 @@ class Plan:
         self.n_new = self.info.n_new
 
     def _rows(self):
-        """Shapes of q and of k_new / v_new, elements of q, torch's storage type and int32: made once (a field of a ctypes
-        struct takes as long as a tensor's check)."""
+        """Shapes of q and of k_new / v_new, elements of q, torch's storage type and int32, (head_dim, dtype): made once (a field
+        of a ctypes struct takes as long as a tensor's check)."""
         if self._dims is None:
             import torch
             sh = self.shape
             shapes = [torch.Size((self.n_new, h, sh.head_dim)) for h in (sh.n_q_heads, sh.n_kv_heads)]
-            self._dims = *shapes, shapes[0].numel(), _storage_type(sh), torch.int32
+            self._dims = *shapes, shapes[0].numel(), _storage_type(sh), torch.int32, (sh.head_dim, sh.dtype)
         return self._dims
 
     def update(self, desc, q_pos=None, stream=None) -> None:
@@ -365,6 +365,7 @@ class QkNorm:
                 raise ValueError("weights: head_dim contiguous elements of the storage type")
         self.weights = q_weight, k_weight           # kept alive
         self.n_axes = max(axes) + 1
+        self.made_for = shape.head_dim, shape.dtype
         self.c = _QkNorm(_ptr(q_weight), _ptr(k_weight), eps, self.n_axes, 1 if rotate_q else 0, (ctypes.c_uint8 * 64)(*axes))
         self.address = ctypes.addressof(self.c)
 
@@ -390,7 +391,9 @@ def _token_stride(x, dtype, shape) -> int:
 def qk_norm_append(plan: Plan, norm: QkNorm, q, k_new, v_new, pos, k_pool, v_pool, q_out, stream=None) -> None:
     """Norms, rotation and paged append of the step's new tokens (see ``aspd_qk_norm_append``).  q, k_new, v_new may be
     views of one packed projection; pos: device int32 [n_axes][n_new] (further rows are not read; flat: n_axes * n_new)."""
-    q_shape, kv_shape, q_size, dtype, int32 = plan._rows()
+    q_shape, kv_shape, q_size, dtype, int32, made_for = plan._rows()
+    if norm.made_for != made_for:
+        raise ValueError("norm: made for another head_dim or storage type")
     n, rows = q_shape[0], pos.shape
     if not (rows[1] == n and rows[0] >= norm.n_axes if len(rows) == 2 else len(rows) == 1 and rows[0] == norm.n_axes * n) or \
             pos.dtype is not int32 or not pos.is_contiguous():

@@ -49,3 +49,11 @@ def test_gains_are_of_the_storage_type(dtype, others):
                 B.QkNorm(c.shape, **{name: torch.ones(64, dtype=other)})
     with pytest.raises(B.AspdError):
         c(B.QkNorm(c.shape, torch.ones(64, dtype=c.dt), torch.ones(64, dtype=c.dt)), torch.zeros(1, c.n, dtype=torch.int32))
+
+
+def test_a_norm_made_for_another_shape():
+    """Its gains would be read beyond their end, or as another type."""
+    c = Call()
+    for other in (Call("f32"), Call("bf16", 128)):
+        with pytest.raises(ValueError):
+            c(B.QkNorm(other.shape, torch.ones(other.shape.head_dim, dtype=other.dt)), torch.zeros(1, c.n, dtype=torch.int32))
