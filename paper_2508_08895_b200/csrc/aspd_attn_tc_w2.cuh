@@ -355,13 +355,13 @@ __device__ __forceinline__ void softmax_group_w2(const Ctx& c, MiscW2* misc, uin
 
 
 // A thread's 32 scores of a half that reach beyond the short polynomial, 16 at a time out of tensor memory and their P back over scores
-// that have been read (P of scores 16 i ... takes columns 8 i ...): the longer polynomial up to the cap, two more special functions a score
-// beyond.  Returned: the row's sum.  A loop, and a short one, on purpose: the passes are straight code, and forms of
-// them taken in turn did not fit the instruction cache (products up to the cap and beyond it in one step, a quarter more passes, were
-// three times the time).
+// that have been read (P of scores 16 i ... takes columns 8 i ...): the polynomial with its bend up to the cap, two more special functions a
+// score beyond.  Returned: the row's sum.  masked (uniform): some row of the warp does not see all 32 keys.  A loop, and a short one, on
+// purpose: the passes are straight code, and forms of them taken in turn did not fit the instruction cache (products up to the cap
+// and beyond it in one step, a quarter more passes, were three times the time).
 template <bool BIAS>
 __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, const RowBias& rb, const int4& vis, uint32_t s_addr, int ring, int page0, int kb0,
-                                            float& top) {
+                                            bool masked, float& top) {
   float2 sum = make_float2(0.f, 0.f);
   top = 0.f;
 #pragma unroll 1
@@ -370,41 +370,35 @@ __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, co
     ASPD_TMEM_LD16(s_addr + q * 16, s, 0);
     const int nv = misc->nval[ring][page0 + q] & 255, kb = kb0 + q * 16;
     const uint32_t mask = bits_between(0, min(nv, vis.x - kb)) | bits_between(vis.y - kb, min(nv, vis.z - kb));
-    float2 dist = make_float2(0.f, 0.f);
-    if constexpr (BIAS) {
-      dist.x = (float)(misc->kpos[ring][page0 + q] - rb.pos);
-      dist.y = dist.x + 1.f;
-    }
+    float dist = 0.f;
+    if constexpr (BIAS) dist = (float)(misc->kpos[ring][page0 + q] - rb.pos);
     tmem_wait_ld16(s);
+    if (masked) {                                  // what the row does not see sends nobody here, nor on to the special functions
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (mask >> i) & 1u ? s[i] : 0.f;
+    }
     float mx = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) mx = fmaxf(mx, fmaxf(fabsf(s[i]), fabsf(s[i + 1])));
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fabsf(s[i]));
     top = fmaxf(top, mx);
-    if (__any_sync(0xffffffffu, mx > c.sp.poly_limit)) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = saturated(s[i], c.sp);
+    const bool beyond = __any_sync(0xffffffffu, mx > c.sp.poly_limit) != 0;
+    if constexpr (BIAS) {
+      auto bias = [&](int i) {
+        return __fmul2_rn(make_float2(rb.slope, rb.slope), __fadd2_rn(make_float2(dist, dist), make_float2((float)i, (float)(i + 1))));
+      };
+      cap_far(s, c.sp, beyond, WithBias<decltype(bias)>{bias});
     } else {
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float2 z = __fmul2_rn(make_float2(s[i], s[i + 1]), make_float2(c.sp.cap_in, c.sp.cap_in)), u = __fmul2_rn(z, z);
-        float2 p = make_float2(c.sp.poly[5], c.sp.poly[5]);
-#pragma unroll
-        for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.poly[k], c.sp.poly[k]));
-        p = __fmul2_rn(p, z);
-        s[i] = p.x; s[i + 1] = p.y;
-      }
+      cap_far(s, c.sp, beyond, NoBias());
     }
     uint32_t p8[8];
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      float2 x = make_float2(s[i], s[i + 1]);
-      if constexpr (BIAS) {
-        x = __ffma2_rn(make_float2(rb.slope, rb.slope), dist, x);
-        dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
-      }
-      p8[i >> 1] = pack_bf16(ex2((mask >> i) & 1u ? x.x : -INFINITY), ex2((mask >> (i + 1)) & 1u ? x.y : -INFINITY));
-      sum = __fadd2_rn(sum, unpack_bf16(p8[i >> 1]));
+    for (int i = 0; i < 16; i += 2) p8[i >> 1] = pack_bf16(ex2(s[i]), ex2(s[i + 1]));
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) p8[i >> 1] &= ((mask >> i) & 1u ? 0xffffu : 0u) | ((mask >> (i + 1)) & 1u ? 0xffff0000u : 0u);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = __fadd2_rn(sum, unpack_bf16(p8[i]));
     ASPD_TMEM_ST8U(s_addr + q * 8, p8);
   }
   return sum.x + sum.y;
@@ -500,11 +494,12 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
               float2 x = make_float2(s[pg * 16 + i], s[pg * 16 + i + 1]);
+              if (MASKED && mask != 0xFFFFu) {       // (columns behind the item's last page hold an earlier half's scores or P)
+                x.x = (mask >> i) & 1u ? x.x : 0.f;
+                x.y = (mask >> (i + 1)) & 1u ? x.y : 0.f;
+              }
               top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
-              const float2 u = __fmul2_rn(x, x);
-              float2 p = make_float2(c.sp.near[3], c.sp.near[3]);
-#pragma unroll
-              for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(c.sp.near[k], c.sp.near[k]));
+              const float2 p = cap_short(__fmul2_rn(x, x), c.sp);
               if constexpr (BIAS) {
                 x = __ffma2_rn(x, p, __fmul2_rn(make_float2(rb.slope, rb.slope), dist));
                 dist = __fadd2_rn(dist, make_float2(2.f, 2.f));
@@ -531,7 +526,7 @@ __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc,
           again = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
         }
         if (again) {
-          sum = far_scores<BIAS>(c, misc, rb, vis, s_base + h * 64, ring, page0, kb0, top);
+          sum = far_scores<BIAS>(c, misc, rb, vis, s_base + h * 64, ring, page0, kb0, masked, top);
           far = __any_sync(0xffffffffu, top > c.sp.near_limit) != 0;
         } else {
           ASPD_TMEM_ST16U(s_base + h * 64, pk);

@@ -4,6 +4,8 @@
 // scale of 1.
 #pragma once
 
+#include <type_traits>
+
 #include "aspd_internal.cuh"
 
 namespace aspd {
@@ -12,19 +14,22 @@ namespace {
 struct ScoreParams {
   float scale;             // of the products, in log2 units
   float cap_in, cap_out;   // sm_scale / cap and cap * log2(e); 0: scores are not capped
-  float poly[6];           // of cap * tanh(z) / z in z^2, |z| <= 1, log2 units
-  float poly_limit;        // products up to that magnitude have |z| <= 1
   float near[4], near_limit;   // of cap * tanh(z) / product in the product's square, |z| <= 0.6, log2 units; up to that magnitude
+  float bend[4], bend_in;  // what comes to it beyond, in z^2 - 0.36; (sm_scale / cap)^2
+  float poly[6];           // caps far from sm_scale (near_limit = 0): of cap * tanh(z) / z in z^2, |z| <= 1, log2 units
+  float poly_limit;        // products up to that magnitude have |z| <= 1.1 (caps far from sm_scale: 1), which the polynomials reach
 };
-// tanh(z) / z as a polynomial in z^2 of degree 5 on |z| <= 1 and of degree 3 on |z| <= 0.6, fitted for the least largest relative
-// error (Lawson's iteration of weighted least squares on Chebyshev points): 6.5e-7 and 2.3e-6 with their fp32 evaluation.
+// tanh(z) / z in z^2, fitted for the least largest relative error.  kTanhShort: degree 3, |z| <= 0.6 (Lawson's iteration of weighted least
+// squares on Chebyshev points), 2.3e-6 with its fp32 evaluation.  kTanhBend: t (b0 + b1 t + b2 t^2 + b3 t^3), t = max(z^2 - 0.36, 0), on top of
+// it to |z| = 1.1 (linear programming on Chebyshev points), 2.3e-6.  kTanh: degree 5, |z| <= 1, 6.5e-7.
 inline ScoreParams score_params(const aspd_plan* p) {
   constexpr double kLog2E = 1.4426950408889634;
   constexpr double kTanh[6] = {0.9999994039535522, -0.3332904279232025, 0.13281434774398804, -0.051605675369501114, 0.016743116080760956,
                                -0.0030670601408928633};
   constexpr double kTanhShort[4] = {0.9999978513027259, -0.33314039269087015, 0.1305785620279237, -0.04092942321980133};
+  constexpr double kTanhBend[4] = {0.00028090211918264534, 0.0012360130940150202, 0.013265232803973168, 0.005514669593634999};
   const double s = p->shape.sm_scale, c = p->cap;
-  ScoreParams sp = {(float)(s * kLog2E), 0.f, 0.f, {}, 0.f, {}, 0.f};
+  ScoreParams sp = {(float)(s * kLog2E)};
   if (c > 0) {
     sp.cap_in = (float)(s / c);
     sp.cap_out = (float)(c * kLog2E);
@@ -32,64 +37,116 @@ inline ScoreParams score_params(const aspd_plan* p) {
     for (int k = 0; k < 6; ++k) sp.poly[k] = (float)(kTanh[k] * c * kLog2E);
     // the powers of sm_scale / cap in the coefficients: as far as they are ordinary fp32 numbers
     const double z = s / c;
-    if (z > 1e-5 && z < 1e5) sp.near_limit = (float)(0.6 / z);
-    for (int k = 0; k < 4; ++k) sp.near[k] = sp.near_limit > 0.f ? (float)(kTanhShort[k] * s * kLog2E * pow(z, 2 * k)) : 0.f;
+    if (z > 1e-5 && z < 1e5) {
+      sp.near_limit = (float)(0.6 / z);
+      sp.poly_limit = (float)(1.1 / z);
+      sp.bend_in = (float)(z * z);
+      for (int k = 0; k < 4; ++k) sp.near[k] = (float)(kTanhShort[k] * s * kLog2E * pow(z, 2 * k));
+      for (int k = 0; k < 4; ++k) sp.bend[k] = (float)(kTanhBend[k] * s * kLog2E);
+    }
   }
   return sp;
 }
 
-// cap * tanh(z), z = product * sm_scale / cap, in log2 units.  Up to |z| = 1 the polynomial; beyond, tanh|z| = 1 - 2 / (2^(2 |z|
-// log2 e) + 1), exact at its end (the exponential may overflow), off by 2^-22 of itself.  Either way a logit is off by less than 3e-6
-// of itself (7e-5 for a score of 30), far below what the rounding of queries and weights to bf16 does.
+// cap * tanh(z), z = product * sm_scale / cap, in log2 units: up to |z| = 0.6 the short polynomial of the product, up to 1.1 with its
+// bend; beyond, tanh|z| = 1 - 2 / (2^(2 |z| log2 e) + 1), exact at its end (the exponential may overflow), off by 2^-22 of itself.
+// Either way a logit is off by less than 3e-6 of itself (7e-5 for a score of 30), far below what the rounding of queries and
+// weights to bf16 does.
 //
-// saturated: the second form for any z, off by 2^-22 of the cap (near 0 its subtraction costs relative, not absolute, precision).
+// What a score becomes is a matter of that score alone (a bend of 0 leaves the short polynomial bit for bit), so that a row's bits
+// do not depend on the keys that it does not see, on the rows beside it, or on what an earlier step left in columns without
+// scores.  Votes only leave out what no score of the warp needs.
+__device__ __forceinline__ float2 cap_short(float2 u, const ScoreParams& sp) {      // (without the factor x; u = x^2)
+  float2 p = make_float2(sp.near[3], sp.near[3]);
+#pragma unroll
+  for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(sp.near[k], sp.near[k]));
+  return p;
+}
+__device__ __forceinline__ float2 cap_bent(float2 u, const ScoreParams& sp) {
+  float2 t = __ffma2_rn(u, make_float2(sp.bend_in, sp.bend_in), make_float2(-0.36f, -0.36f));
+  t = make_float2(fmaxf(t.x, 0.f), fmaxf(t.y, 0.f));
+  float2 b = make_float2(sp.bend[3], sp.bend[3]);
+#pragma unroll
+  for (int k = 2; k >= 0; --k) b = __ffma2_rn(b, t, make_float2(sp.bend[k], sp.bend[k]));
+  return __ffma2_rn(b, t, cap_short(u, sp));
+}
+__device__ __forceinline__ float2 cap_whole(float2 u, const ScoreParams& sp) {      // (without z; u = z^2)
+  float2 p = make_float2(sp.poly[5], sp.poly[5]);
+#pragma unroll
+  for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(sp.poly[k], sp.poly[k]));
+  return p;
+}
 __device__ __forceinline__ float saturated(float s, const ScoreParams& sp) {
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(s * sp.cap_in * 2.885390081777927f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
+  // (volatile: not in a branch of its own for each score)
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(s * sp.cap_in * 2.885390081777927f));
+  asm volatile("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
   return fmaf(-2.f * sp.cap_out, r, sp.cap_out);
 }
-__device__ __forceinline__ float capped(float s, const ScoreParams& sp) {
-  const float z = s * sp.cap_in, u = z * z;
-  float p = sp.poly[5], e, r;
+// What the end of a capped score is: nothing; a bias is added in the polynomials' last step (bias(i): of scores i, i + 1).
+struct NoBias {
+  __device__ __forceinline__ float2 times(float2 x, float2 p, int) const { return __fmul2_rn(x, p); }
+  __device__ __forceinline__ float2 plus(float2 y, int) const { return y; }
+};
+template <typename F>
+struct WithBias {
+  F bias;
+  __device__ __forceinline__ float2 times(float2 x, float2 p, int i) const { return __ffma2_rn(x, p, bias(i)); }
+  __device__ __forceinline__ float2 plus(float2 y, int i) const { return __fadd2_rn(y, bias(i)); }
+};
+template <int N, typename End>
+__device__ __forceinline__ void cap_near(float (&s)[N], const ScoreParams& sp, const End& end) {
 #pragma unroll
-  for (int k = 4; k >= 0; --k) p = fmaf(p, u, sp.poly[k]);
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(z) * 2.885390081777927f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
-  return fabsf(z) <= 1.f ? z * p : copysignf(fmaf(-2.f * sp.cap_out, r, sp.cap_out), z);
+  for (int i = 0; i < N; i += 2) {
+    const float2 x = make_float2(s[i], s[i + 1]), y = end.times(x, cap_short(__fmul2_rn(x, x), sp), i);
+    s[i] = y.x; s[i + 1] = y.y;
+  }
 }
-// N scores of a thread: where none passes |z| = 0.6, or 1, packed fp32 pairs and no special-function
-// unit, which the softmax's own exponentials keep busy already (the two-tile kernel, 17 k query tokens: 1 496 us a layer with two more special
-// functions a score, 982 with the polynomial).
+// any_beyond (uniform): whether some score of the warp is beyond the polynomials' reach
+template <int N, typename End>
+__device__ __forceinline__ void cap_far(float (&s)[N], const ScoreParams& sp, bool any_beyond, const End& end) {
+  auto all = [&](auto whole, auto beyond) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 x = make_float2(s[i], s[i + 1]);
+      float2 y;
+      if constexpr (decltype(whole)::value) {
+        const float2 z = __fmul2_rn(x, make_float2(sp.cap_in, sp.cap_in));
+        y = end.times(z, cap_whole(__fmul2_rn(z, z), sp), i);
+      } else {
+        y = end.times(x, cap_bent(__fmul2_rn(x, x), sp), i);
+      }
+      if constexpr (decltype(beyond)::value) {
+        const float2 e = end.plus(make_float2(saturated(x.x, sp), saturated(x.y, sp)), i);
+        y.x = fabsf(x.x) <= sp.poly_limit ? y.x : e.x;
+        y.y = fabsf(x.y) <= sp.poly_limit ? y.y : e.y;
+      }
+      s[i] = y.x; s[i + 1] = y.y;
+    }
+  };
+  if (sp.near_limit == 0.f) all(std::true_type(), std::true_type());
+  else if (any_beyond) all(std::false_type(), std::true_type());
+  else all(std::false_type(), std::false_type());
+}
+__device__ __forceinline__ float capped(float s, const ScoreParams& sp) {
+  float x[2] = {s, 0.f};
+  cap_far(x, sp, true, NoBias());
+  return x[0];
+}
+// N scores of a thread, the whole warp together, 16 at a time: mostly none passes |z| = 0.6, or 1.1, and packed fp32 pairs do without the
+// special-function unit, which the softmax's own exponentials keep busy already.
 template <int N>
 __device__ __forceinline__ void cap_scores(float (&s)[N], const ScoreParams& sp) {
-  float mx = 0.f;
+  constexpr int M = N < 16 ? N : 16;
 #pragma unroll
-  for (int i = 0; i < N; i += 2) mx = fmaxf(mx, fmaxf(fabsf(s[i]), fabsf(s[i + 1])));
-  if (mx <= sp.near_limit) {
+  for (int j = 0; j < N; j += M) {
+    float x[M], mx = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      const float2 x = make_float2(s[i], s[i + 1]), u = __fmul2_rn(x, x);
-      float2 p = make_float2(sp.near[3], sp.near[3]);
+    for (int i = 0; i < M; ++i) { x[i] = s[j + i]; mx = fmaxf(mx, fabsf(x[i])); }
+    if (!__any_sync(0xffffffffu, mx > sp.near_limit)) cap_near(x, sp, NoBias());
+    else cap_far(x, sp, __any_sync(0xffffffffu, mx > sp.poly_limit) != 0, NoBias());
 #pragma unroll
-      for (int k = 2; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(sp.near[k], sp.near[k]));
-      p = __fmul2_rn(p, x);
-      s[i] = p.x; s[i + 1] = p.y;
-    }
-  } else if (mx <= sp.poly_limit) {
-    const float2 in = make_float2(sp.cap_in, sp.cap_in);
-#pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      const float2 z = __fmul2_rn(make_float2(s[i], s[i + 1]), in), u = __fmul2_rn(z, z);
-      float2 p = make_float2(sp.poly[5], sp.poly[5]);
-#pragma unroll
-      for (int k = 4; k >= 0; --k) p = __ffma2_rn(p, u, make_float2(sp.poly[k], sp.poly[k]));
-      p = __fmul2_rn(p, z);
-      s[i] = p.x; s[i + 1] = p.y;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = capped(s[i], sp);
+    for (int i = 0; i < M; ++i) s[j + i] = x[i];
   }
 }
 
