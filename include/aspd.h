@@ -125,8 +125,11 @@ typedef struct {
   int32_t wide_rows;    /* plans that deal whole streams to the tensor-core kernel: query rows of a row
                            block, 128 (one tile) or 256 (two tiles scored against every K/V tile the CTA
                            fetches); 0 = automatic (256 when a request has more query tokens than one
-                           tile holds).  Scores capped above 55 or capped with a bias that raises any:
-                           never 256, and cut instead of dealt unless queries come rotated (aspd_scores_t)      */
+                           tile holds).  Capped scores take 256 with weights against a fixed reference only
+                           (caps up to 55, no bias that raises a score).  Where the attention rotates the queries,
+                           capped plans of heads of 128 in pages of 16 are dealt in row blocks of 256 or not at all:
+                           asked for 128, or with 0 where every request fits one tile, they are cut (streams of
+                           64 rows; aspd_plan_info_t.dealt says what a plan is)                      */
   int32_t mma_m;        /* stream-K plans of the tensor-core kernel: M of its MMAs, 128 (the at most 64 query
                            rows of a row block are replicated to fill 128 accumulator rows), 64 (half the
                            tensor work; the accumulators then use 16 lanes of each quadrant) or 96, which

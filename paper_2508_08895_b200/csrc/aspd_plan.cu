@@ -695,7 +695,7 @@ static int plan_create_impl(const aspd_shape_t* shape, const aspd_request_t* req
                       (long)streams.size() >= 2L * ctas_for(total_pages) && (tune.n_ctas > 0 || ctas_for(total_pages) >= p->sm_count);
   if (deal_streams && (long)streams.size() < 4L * ctas_for(total_pages)) deal_streams = !coarse && deal_out(ctas_for(total_pages)) <= kDealSkew;
   // Capped scores of queries that the attention rotates: those come in two pieces, for which the one-tile variant has no room.  Such
-  // streams are dealt to the two-tile kernel or cut.
+  // streams are dealt to the two-tile kernel or cut, where row blocks of 128 are asked for too.
   if (deal_streams && cap > 0.f && !rotated && kernel == ASPD_KERNEL_MMA && wide_ok) {
     int most_q = 0;
     for (const Block& bk : blocks) most_q = std::max(most_q, bk.n_tok);
