@@ -688,8 +688,10 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
     }
   } else if constexpr (CAPPED) {
     // ============================ MMA issuers, capped scores (warp 18: group 0, warp 19: group 1) ============================
-    // As below, by halves of 64 keys with a stage each: P.V of half v as soon as its P is there, scores of half v + 2 right behind, which
-    // go over it.  Scores are two products where the queries come in two pieces.
+    // As below, by halves of 64 keys with a stage each: P.V of half v as soon as its P is there, then scores of half v + 2, which go
+    // over that P once the P.V has read it: a word says so (two products that differ in shape and accumulator have no order of their
+    // own).  The group is in its pass over half v + 1 meanwhile; us a layer with and without the word, 17 k query tokens, queries that come
+    // rotated 877 and 911, in two pieces 1 064 and 1 118.  Scores are two products where the queries come in two pieces.
     const int grp = warp - W2_ISSUE;
     const uint32_t fm = 0xffffffffu;
     const uint32_t tmem_u = __shfl_sync(fm, tmem, 0), base_u = __shfl_sync(fm, base, 0), bars_u = base_u + W2_OFF_MISC;
@@ -700,7 +702,8 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
     const uint32_t s_tmem = tmem_u + COL_S + grp * 128, o_tmem = tmem_u + COL_O + grp * 128;
     const uint64_t adesc_q = smem_desc(base_u + W2C_OFF_Q + grp * kTileBytes, 16, 1024), adesc_q2 = smem_desc(base_u + W2C_OFF_Q + (2 + grp) * kTileBytes, 16, 1024);
     const uint32_t bar_sfull = bars_u + 8 * (WS_FULL + 2 * grp), bar_pfull = bars_u + 8 * (WP_FULL + 2 * grp);
-    int gbase = 0, ic = 0, cnt_p[2] = {0, 0};          // halves of the items so far; the group's items and P's (by buffer) so far
+    const uint32_t bar_pvdone = bars_u + 8 * (WPV_DONE + grp);
+    int gbase = 0, ic = 0, cnt_p[2] = {0, 0}, cnt_pv = 0;          // halves of the items so far; the group's items and P's (by buffer) so far
     bool ok = true;
     for (int idx = ib; idx < ie && ok; ++idx) {
       const DeviceItem it = get_item_w2(c, misc, idx, ib);
@@ -729,6 +732,7 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
           }
         }
         ok = ok && wait_all(bars_u + 8 * (WQ_FULL + grp), ic & 1);
+        if (ic > 0) { ok = ok && wait_all(bar_pvdone, cnt_pv & 1); ++cnt_pv; }      // the last item's last P is read
         ++ic;
         for (int v = 0; v < min(2, n_halves) && ok; ++v) {
           ok = there(WK_FULL, v);
@@ -745,9 +749,16 @@ __global__ void __launch_bounds__(kThreadsW2<SC>, 1) attn_tc_w2_kernel(Ctx c) {
           tc_fence_after();
           tc_mma_ts_pv_lane0<32>(o_tmem, s_tmem + b * 64, smem_desc(base_u + W2C_OFF_V + st * kStageW2c, 1024, 2048), idesc_pv, v > 0 ? 1u : 0u,
                                  min(4, n_pages - 4 * v));
-          if (v + 2 < n_halves) issue_s(v + 2);
+          if (v + 2 < n_halves || v == n_halves - 1) tc_commit_lane0(bar_pvdone);
           if (v == n_halves - 1) tc_commit_lane0(bars_u + 8 * (WO_FULL + grp));
           release(bars_u + 8 * (WV_EMPTY + st));
+          if (v + 2 < n_halves) {                      // its scores go over the P that the P.V reads
+            ok = wait_all(bar_pvdone, cnt_pv & 1);
+            ++cnt_pv;
+            if (!ok) break;
+            tc_fence_after();
+            issue_s(v + 2);
+          }
         }
       }
       if (grp == 0 && lane == 0) *lead = idx + 1;
