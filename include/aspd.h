@@ -278,6 +278,9 @@ typedef struct {
  * negative, above 1e30, or below sm_scale / 1e30; for slopes above 32 in magnitude or not finite; for q_pos with
  * rotated.  ASPD_ERR_UNSUPPORTED for a cap or slopes with tuning->mma_m = 64.  With slopes, ASPD_ERR_TOO_LARGE for
  * position IDs of 2^24 and more.
+ * Logits are fp32 numbers: a bias of b is rounded by up to b * 2^-24, which a key beside its query does not notice and the far
+ * keys of a rising bias (slopes below 0) do: 0.004 at a bias of 65 536.  An infinity in a query, or in a key that a row sees,
+ * makes a capped score of +-cap or NaN.
  */
 int aspd_plan_create_scores(const aspd_shape_t* shape, const aspd_request_t* req, const aspd_branch_t* br,
                             const int32_t* page_ids, int n_req, int64_t n_pool_pages, int mode,
@@ -361,8 +364,9 @@ typedef struct {
  *   RoPE: pair i of a head turned by pos[axis_of_pair[i]][t] * theta^(-2i/head_dim); keys always, queries
  *   with rotate_q
  * and the queries go to q_out, keys and values into the paged cache at the slots of the plan (as
- * aspd_kv_append).  Sums, norms and rotation are fp32 with the angle reduced in fp64; one rounding to the
- * storage type at the end.  The attention call of the same plan reads both.
+ * aspd_kv_append).  Sums, norms and rotation are fp32 with the angle reduced in fp64 (the squares of a head's
+ * elements have to sum up inside fp32's range: elements up to 1e18); one rounding to the storage type at
+ * the end.  The attention call of the same plan reads both.
  *   q, k_new, v_new  rows of n_q_heads / n_kv_heads heads, head_dim elements each, lying together; *_stride
  *                    elements from one token to the next (a multiple of 16 bytes, at least a row), so that
  *                    the three may be views of one packed projection
