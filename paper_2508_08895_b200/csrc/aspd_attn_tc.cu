@@ -366,7 +366,7 @@ __device__ __forceinline__ bool softmax_item(const Ctx& c, const DeviceItem& it,
 // exactly, and where it is nearly all of the sum its rounding would be the output's.  Outputs off from 64 bits (relative, root mean square; 0.0017 is
 // their own rounding): logits with a deviation of 5, 0.0019, of 9, 0.0016 to 0.0017; with the sum of unrounded weights 0.0023, and 0.0022 to 0.0029.
 // With moving references and this one, us a layer: one request of 2 k tokens 7.6 and 7.1 (plain scores 7.2), 32 requests 47.5 and
-// 46.9 (46.7), the same with scores beyond 0.6 of a cap of 20 58 and 48.
+// 46.9 (46.7); the same with a cap of 20, where one score in sixty is beyond 0.6 of it, 58 and 50.
 template <int NC>
 __device__ __forceinline__ bool softmax_item_fixed(const Ctx& c, const DeviceItem& it, Misc* misc, uint32_t bars, uint32_t smem_p, uint32_t tmem,
                                                    int item_no, int& g) {

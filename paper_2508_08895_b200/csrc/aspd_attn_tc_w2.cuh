@@ -406,12 +406,13 @@ __device__ __forceinline__ float far_scores(const Ctx& c, const MiscW2* misc, co
 
 // Capped scores, with fixed references only (aspd_plan::fixed_ref): the exponentials are taken against 0 always, so that nothing but the
 // sums goes from key to key, and a row is two threads': eight warps to a group, thread (part, r) takes 32 of the 64 scores of
-// a half.  17 k query tokens of 32 requests, a cap of 50, us a layer below the power cap: 815 with queries that come rotated (plain scores 690 to
-// 730), 1 010 with queries in two pieces, whose scores are two products each; the tensor pipe is busy half of the time, the rest is
+// a half.  17 k query tokens of 32 requests, a cap of 50, us a layer below the power cap: 860 with queries that come rotated (plain scores 735
+// to 745), 1 000 with queries in two pieces, whose scores are two products each; the tensor pipe is busy half of the time, the rest is
 // the way from a half's scores to its P.V.  (Four warps a group, a thread to a row as in softmax_group_w2: 853 instead of 834 under the cap.
-// Two pieces: scores of a whole tile in one product, 1 080 against 1 020 then; the first piece in tensor memory and one buffer of 64 scores, 1 350.)  A half is one pass with the short polynomial, which keeps the largest product; where that turns
-// out to be beyond the polynomial's range (scores above 0.6 of the cap) it is taken again by far_scores, and the warp's next half goes
-// there at once.  Rows are divided by the sum of their rounded weights (see softmax_item_fixed; 2 to 5 % of the time).  P lies over the thread's own scores: 16 columns at columns 0 and 32 of the half's 64.
+// Two pieces: scores of a whole tile in one product, 1 080 against 1 020 then; the first piece in tensor memory and one buffer of 64 scores, 1 350.)
+// A half is one pass with the short polynomial, which keeps the largest product; where that turns out to be beyond the polynomial's range
+// (scores above 0.6 of the cap) it is taken again by far_scores, and the warp's next half goes there at once: 1 290 and 1 340 with a cap of 20,
+// where one score in sixty is beyond 0.6 of it, 1 640 and 1 680 with a cap of 8, where most halves have scores beyond the cap.  Rows are divided by the sum of their rounded weights (see softmax_item_fixed; 2 to 5 % of the time).  P lies over the thread's own scores: 16 columns at columns 0 and 32 of the half's 64.
 template <bool BIAS>
 __device__ __forceinline__ void softmax_group_capped(const Ctx& c, MiscW2* misc, uint32_t bars, uint32_t base, uint32_t tmem, int item_begin,
                                                      int item_end, int grp, int tpt) {

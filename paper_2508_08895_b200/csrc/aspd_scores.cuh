@@ -134,7 +134,8 @@ __device__ __forceinline__ float capped(float s, const ScoreParams& sp) {
   return x[0];
 }
 // N scores of a thread, the whole warp together, 16 at a time: mostly none passes |z| = 0.6, or 1.1, and packed fp32 pairs do without the
-// special-function unit, which the softmax's own exponentials keep busy already.
+// special-function unit, which the softmax's own exponentials keep busy already.  Serving batch of 32 requests, us a layer with queries that come
+// rotated: no cap 46.9, caps of 50 / 20 / 8 (logits with a deviation of 5) 47.5 / 49.6 / 60.8; 47.4 / 50.7 / 64.8 when each thread took its own way.
 template <int N>
 __device__ __forceinline__ void cap_scores(float (&s)[N], const ScoreParams& sp) {
   constexpr int M = N < 16 ? N : 16;
