@@ -36,8 +36,8 @@ inline ScoreParams score_params(const aspd_plan* p) {
     sp.poly_limit = (float)(c / s);
     for (int k = 0; k < 6; ++k) sp.poly[k] = (float)(kTanh[k] * c * kLog2E);
     // the powers of sm_scale / cap in the coefficients: as far as they are ordinary fp32 numbers
-    const double z = s / c;
-    if (z > 1e-5 && z < 1e5) {
+    const double z = s / c, least = s * pow(z, 6);
+    if (z > 1e-5 && z < 1e5 && least > 1e-35 && least < 1e37) {
       sp.near_limit = (float)(0.6 / z);
       sp.poly_limit = (float)(1.1 / z);
       sp.bend_in = (float)(z * z);
