@@ -280,7 +280,8 @@ typedef struct {
  * position IDs of 2^24 and more.
  * Logits are fp32 numbers: a bias of b is rounded by up to b * 2^-24, which a key beside its query does not notice and the far
  * keys of a rising bias (slopes below 0) do: 0.004 at a bias of 65 536.  An infinity in a query, or in a key that a row sees,
- * makes a capped score of +-cap or NaN.
+ * makes a capped score of +-cap or NaN.  Caps up to 55 are taken without a maximum, so that weights lie between e^-cap and e^cap: the
+ * values' sums have to stay inside fp32's range with those (|v| times the number of keys below 1e14, and what is below 1e-14 may be lost).
  */
 int aspd_plan_create_scores(const aspd_shape_t* shape, const aspd_request_t* req, const aspd_branch_t* br,
                             const int32_t* page_ids, int n_req, int64_t n_pool_pages, int mode,
